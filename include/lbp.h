@@ -66,7 +66,7 @@ typedef enum {
   LBP_ERR_CUDA = 9,       /* a CUDA call failed; see lbp_last_cuda_error()      */
   LBP_ERR_TIMEOUT = 10,   /* a bounded device-side wait expired                 */
   LBP_ERR_CAPACITY = 11,  /* output array too small (lbp_select_bases)          */
-  LBP_ERR_OVERLAP = 12    /* buffers of different problems of a batch overlap   */
+  LBP_ERR_OVERLAP = 12    /* buffers of a batch's problems, or of a call, overlap */
 } lbp_status;
 
 typedef enum { LBP_F32 = 0, LBP_BF16 = 1 } lbp_dtype;
@@ -287,6 +287,111 @@ int lbp_backward_projected(const void* x_hat, const void* g_y, const void* W,
 int lbp_backward_fullrank(const void* x, const void* g_y, const void* W,
                           void* g_x, void* g_W, const lbp_layer* layer,
                           void* ws, size_t ws_bytes, void* stream);
+
+/* ---- what a layer does around its product --------------------------------
+ *
+ * The paper's Eq. 1 is the bare product; in a network a bias, an activation,
+ * dropout and the sum with a residual stream follow it:
+ *     z = x W^T + b;      y = residual + drop(act(z));
+ * and the gradient that reaches the product, and so Algorithm 1, is
+ *     g_z = drop(g_y) act'(z).
+ * z is taken in fp32; y and the z that is kept are rounded once.
+ *
+ * drop() keeps no mask: whether an element stays is a function of its number n,
+ * a seed and an offset.  The 16-bit number u(n) is half n % 2 (0: the low one) of
+ * word (n % 8) / 2 of Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011) with the counter (lo(n/8), hi(n/8),
+ * lo(offset), hi(offset) + 2^31) and the key (lo(seed), hi(seed)).  With t = p
+ * 2^16 rounded to the nearest integer,
+ *     drop(v) = v * 2^16 / (2^16 - t) where u(n) >= t, else 0
+ * (p is thus taken to a multiple of 2^-16; t = 0 leaves v as it is, p = 1 leaves
+ * nothing).  A dropped element is 0 whatever it was, an infinity or NaN too.
+ * Calls with the same seed, offset and numbers drop the same elements; other
+ * offsets give other, independent choices.
+ *
+ * A row has C elements; `pitch` arguments are distances between rows in elements
+ * (0: dense rows, C), at least C and with the same alignment as pointers.  Rows of
+ * one tensor may not overlap.  rows = 0 is a call that does nothing. */
+typedef enum {
+  LBP_ACT_NONE = 0,
+  LBP_ACT_RELU = 1,       /* act'(0) = 0                                        */
+  LBP_ACT_GELU = 2,       /* z Phi(z), Phi by the error function                */
+  LBP_ACT_GELU_TANH = 3,  /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))    */
+  LBP_ACT_SILU = 4        /* z / (1 + exp(-z))                                  */
+} lbp_act;
+
+typedef struct {
+  int32_t act;            /* lbp_act                                            */
+  float p;                /* probability of dropping, 0..1 (0: no dropout)      */
+  /* The seed and offset of drop(): *seed_dev instead of seed where that is not
+   * NULL, and *offset_dev + offset where that is not NULL.  The two DEVICE pointers
+   * are read by the kernels, so that a captured graph draws new numbers at every
+   * replay. */
+  uint64_t seed, offset;
+  const uint64_t* seed_dev;
+  const uint64_t* offset_dev;
+  /* NULL, or a DEVICE array of two: the seed and offset that the call has used
+   * are written there (for the seed_dev and offset_dev of its backward pass). */
+  uint64_t* used;
+  /* Number of an element: of element c of row i, first + i * number.token + c; of
+   * element (b, h, w, c) of a token grid, first + b * number.image + h * number.row +
+   * w * number.token + c.  All three zero: dense.  Multiples of 8 with bf16 data, of 4
+   * with fp32. */
+  int64_t first;
+  lbp_view number;
+} lbp_epilogue;
+
+/* Distances between rows, in elements (0: dense). */
+typedef struct {
+  int64_t x, residual, y, z;
+} lbp_pitches;
+
+/* y = residual + drop(act(x W^T + bias)), and z where it is wanted.
+ * x (rows, Cin), W (Cout, Cin), bias (Cout), residual and y (rows, Cout), z (rows, Cout),
+ * all of `dtype`; bias, residual and z may be NULL, and so may pitch (all dense) and
+ * epilogue (no activation, no dropout).  y may be the residual itself (same pointer and
+ * pitch); apart from that nothing the call writes may overlap anything else it is given
+ * (LBP_ERR_OVERLAP).  ws: >= lbp_linear_workspace_bytes(...). */
+size_t lbp_linear_workspace_bytes(long long rows, int Cin, int Cout, int dtype);
+int lbp_linear(const void* x, const void* W, const void* bias, const void* residual, void* y, void* z,
+               long long rows, int Cin, int Cout, int dtype, const lbp_pitches* pitch,
+               const lbp_epilogue* epilogue, void* ws, size_t ws_bytes, void* stream);
+
+/* g_z = drop(g_y) act'(z) on rows of C elements.  z may be NULL without an activation.
+ * pitch->y is that of g_y, pitch->z of z, pitch->x of g_z; g_z may be g_y or z itself. */
+int lbp_linear_grad(const void* g_y, const void* z, void* g_z, long long rows, int C, int dtype,
+                    const lbp_pitches* pitch, const lbp_epilogue* epilogue, void* stream);
+
+/* y = residual + drop(x) on rows of C elements; residual may be NULL.  y may be x or the
+ * residual itself.  The backward pass of drop() is drop() of the gradient.  (The
+ * activation of the epilogue must be LBP_ACT_NONE.) */
+int lbp_dropout(const void* x, const void* residual, void* y, long long rows, int C, int dtype,
+                const lbp_pitches* pitch, const lbp_epilogue* epilogue, void* stream);
+
+/* p(g_z) with g_z = drop(g_y) act'(z): as lbp_project on g_z.  g_y, z (B, H, W, C) with the
+ * strides of `view` (NULL: dense), z may be NULL without an activation.
+ * ws: >= lbp_project_grad_workspace_bytes(...), 0 = invalid shape. */
+size_t lbp_project_grad_workspace_bytes(int B, int H, int W, int C, int k, int r, int dtype);
+int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, int W, int C, int k,
+                     const lbp_basis* set, int r, int dtype, const lbp_view* view,
+                     const lbp_epilogue* epilogue, void* ws, size_t ws_bytes, void* stream);
+
+/* What the backward pass of a layer with an epilogue has beside g_y. */
+typedef struct {
+  lbp_epilogue epilogue;   /* numbers: of the elements of g_y                    */
+  const void* z;           /* laid out as g_y; NULL without an activation        */
+  const void* z_extra;     /* laid out as gy_extra; NULL without one             */
+  int64_t first_extra;     /* element c of extra token i has the number          */
+  int64_t number_extra;    /* first_extra + i * number_extra + c (0: Cout)       */
+} lbp_layer_grad;
+
+/* lbp_backward_ex with g_z = drop(g_y) act'(z) in the place of g_y, for the tokens of the grid and the
+ * extra ones; g_bias is the sum of g_z.  ws: >= lbp_workspace_bytes_act (x_hat: whether the call is
+ * handed x_hat; 0 = invalid arguments). */
+size_t lbp_workspace_bytes_act(const lbp_layer* layer, int r, const lbp_extras* ex, int x_hat);
+int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const void* W, void* g_x, void* g_W,
+                     const lbp_layer* layer, const lbp_basis* set, int r, const lbp_extras* ex,
+                     const lbp_layer_grad* grad, void* ws, size_t ws_bytes, void* stream);
 
 /* No counterpart in the paper: a packaging variant of lbp_backward for callers
  * that cannot allocate device memory.  Examples are a server that handed all

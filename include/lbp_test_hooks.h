@@ -69,7 +69,8 @@ int lbp_test_side_section(int device, int (*inside)(void*), void* arg);
 int lbp_test_per_device(const int* devices, int n, uint8_t* done);
 
 /* sizeof of the structs of include/lbp.h as the library was compiled (which: 0
- * lbp_layer, 1 lbp_extras, 2 lbp_view, 3 lbp_basis; anything else: 0), so that a
+ * lbp_layer, 1 lbp_extras, 2 lbp_view, 3 lbp_basis, 4 lbp_epilogue, 5 lbp_pitches, 6
+ * lbp_layer_grad; anything else: 0), so that a
  * binding in another language can check its own declarations against them. */
 size_t lbp_test_struct_size(int which);
 

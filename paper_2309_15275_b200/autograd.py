@@ -41,12 +41,23 @@ class LbpLinear(torch.nn.Module):
 
     `bases` is an ordered list of 0-based (i, j) sequency pairs, e.g. from
     `lbp_select_bases(k, SEL_L1, m)` (Eq. 8) or `lbp_select_lhe` (Sec. 3.2).
+
+    `activation` (one of `ACTIVATIONS`), `dropout` (the probability, drawn from torch's
+    generator of the device while the module is in training mode) and the `residual` given
+    to a call are applied in the product's epilogue.  Such a call wants CUDA tensors of one
+    dtype (fp32 or bf16; under autocast everything is cast to its type).  A backward pass
+    can be captured into a graph like that of torch's own layers, and under the same
+    condition: no graph of earlier, uncaptured passes over the same parameters is alive.
     """
 
     def __init__(self, in_features: int, out_features: int, k: int,
                  bases: Sequence[Tuple[int, int]], device=None, dtype=None, bias: bool = False,
-                 save_projected: bool = False, grid=None):
+                 save_projected: bool = False, grid=None, activation=None, dropout: float = 0.0):
         super().__init__()
+        if activation is not None and activation not in _b.ACTIVATIONS:
+            raise ValueError(f"activation is one of {_b.ACTIVATIONS}, got {activation!r}")
+        if not 0.0 <= float(dropout) <= 1.0:
+            raise ValueError(f"dropout is a probability, got {dropout}")
         w = torch.empty((out_features, in_features), device=device, dtype=dtype)
         torch.nn.init.normal_(w, std=in_features ** -0.5)
         self.weight = torch.nn.Parameter(w)
@@ -55,7 +66,12 @@ class LbpLinear(torch.nn.Module):
         self.k, self.bases = int(k), [tuple(p) for p in bases]
         self.save_projected = bool(save_projected)
         self.grid = None if grid is None else (int(grid[0]), int(grid[1]))
+        self.activation, self.dropout = (None if activation == "none" else activation), float(dropout)
 
-    def forward(self, x: torch.Tensor) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None) -> torch.Tensor:
         H, W = self.grid or (0, 0)
+        p = self.dropout if self.training else 0.0
+        if self.activation is not None or p > 0.0 or residual is not None:
+            return _b._native().layer(x, self.weight, self.bias, residual, self.k, self.bases, self.save_projected,
+                                      H, W, self.activation, p)
         return _b._native().linear(x, self.weight, self.bias, self.k, self.bases, self.save_projected, H, W)

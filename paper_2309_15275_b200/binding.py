@@ -56,6 +56,21 @@ class Extras(C.Structure):
                 ("gx_extra_pitch", C.c_int64)]
 
 
+class Epilogue(C.Structure):
+    _fields_ = [("act", C.c_int32), ("p", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("seed_dev", C.c_void_p), ("offset_dev", C.c_void_p), ("used", C.c_void_p),
+                ("first", C.c_int64), ("number", View)]
+
+
+class Pitches(C.Structure):
+    _fields_ = [("x", C.c_int64), ("residual", C.c_int64), ("y", C.c_int64), ("z", C.c_int64)]
+
+
+class LayerGrad(C.Structure):
+    _fields_ = [("epilogue", Epilogue), ("z", C.c_void_p), ("z_extra", C.c_void_p),
+                ("first_extra", C.c_int64), ("number_extra", C.c_int64)]
+
+
 _LIB = None
 
 
@@ -117,6 +132,22 @@ def _lib() -> C.CDLL:
         lib.lbp_backward_static.argtypes = [vp, vp, vp, vp, vp, C.POINTER(Layer), C.POINTER(Basis),
                                             i32, vp]
         lib.lbp_backward_static.restype = i32
+        i64, ep, pt = C.c_longlong, C.POINTER(Epilogue), C.POINTER(Pitches)
+        lib.lbp_linear_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        lib.lbp_linear_workspace_bytes.restype = sz
+        lib.lbp_linear.argtypes = [vp] * 6 + [i64, i32, i32, i32, pt, ep, vp, sz, vp]
+        for name in ("lbp_linear_grad", "lbp_dropout"):
+            getattr(lib, name).argtypes = [vp, vp, vp, i64, i32, i32, pt, ep, vp]
+        lib.lbp_project_grad_workspace_bytes.argtypes = [i32] * 7
+        lib.lbp_project_grad_workspace_bytes.restype = sz
+        lib.lbp_project_grad.argtypes = [vp, vp, vp] + [i32] * 5 + [C.POINTER(Basis), i32, i32, C.POINTER(View),
+                                                                    ep, vp, sz, vp]
+        lib.lbp_workspace_bytes_act.argtypes = [C.POINTER(Layer), i32, C.POINTER(Extras), i32]
+        lib.lbp_workspace_bytes_act.restype = sz
+        lib.lbp_backward_act.argtypes = [vp] * 6 + [C.POINTER(Layer), C.POINTER(Basis), i32, C.POINTER(Extras),
+                                                    C.POINTER(LayerGrad), vp, sz, vp]
+        for name in ("lbp_linear", "lbp_linear_grad", "lbp_dropout", "lbp_project_grad", "lbp_backward_act"):
+            getattr(lib, name).restype = i32
         lib.lbp_test_tile_plan.argtypes = [i32] * 9 + [C.POINTER(C.c_int32), C.POINTER(C.c_uint16),
                                                        C.POINTER(C.c_uint16)]
         lib.lbp_test_tile_plan.restype = i32
@@ -180,7 +211,8 @@ EXPORTED = ("lbp_select_bases", "lbp_basis_matrix", "lbp_flops", "lbp_status_str
             "lbp_test_reload_env", "lbp_workspace_bytes_ex", "lbp_workspace_bytes_projected", "lbp_backward_ex",
             "lbp_backward_projected", "lbp_test_tile_plan", "lbp_test_struct_size",
             "lbp_test_side_section", "lbp_test_per_device", "lbp_test_products_plan",
-            "lbp_test_float_plan")
+            "lbp_test_float_plan", "lbp_linear_workspace_bytes", "lbp_linear", "lbp_linear_grad", "lbp_dropout",
+            "lbp_project_grad_workspace_bytes", "lbp_project_grad", "lbp_workspace_bytes_act", "lbp_backward_act")
 
 
 def _check(status: int, where: str) -> None:
@@ -230,6 +262,8 @@ def _dev_view(t: torch.Tensor, name: str):
     tok = t.stride(2) if Wd > 1 else Cc
     row = t.stride(1) if H > 1 else Wd * tok
     img = t.stride(0) if B > 1 else H * row
+    if img == row == tok == 0:      # (would read as dense)
+        raise ValueError(f"{name}: its tokens overlap (an expanded tensor?)")
     return t.data_ptr(), (img, row, tok)
 
 
@@ -241,6 +275,8 @@ def _dev_rows(t: torch.Tensor, name: str):
         return t.data_ptr(), 0
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the channels of a token must be contiguous")
+    if t.shape[0] > 1 and t.stride(0) == 0:   # (would read as dense)
+        raise ValueError(f"{name}: its tokens overlap (an expanded tensor?)")
     return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0)
 
 
@@ -616,6 +652,276 @@ def lbp_backward_fullrank(x, g_y, W, k: int, *, gw_dtype: torch.dtype = torch.fl
                                         _dev(g_x, "g_x"), _dev(g_W, "g_W"), C.byref(lay),
                                         _dev(ws, "ws"), ws.numel(), _stream()),
            "lbp_backward_fullrank")
+    return g_x, g_W
+
+
+# ------------------------------------------ what a layer does around its product ----
+ACTIVATIONS = ("none", "relu", "gelu", "gelu_tanh", "silu")
+
+
+def _act_code(activation) -> int:
+    if activation is None:
+        return 0
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation is one of {ACTIVATIONS}, got {activation!r}")
+    return ACTIVATIONS.index(activation)
+
+
+def _epilogue(activation, p, seed, offset, rng, dev) -> Epilogue:
+    e = Epilogue()
+    e.act = _act_code(activation)
+    if not 0.0 <= float(p) <= 1.0:
+        raise ValueError(f"p is a probability, got {p}")
+    e.p = float(p)
+    for name, v in (("seed", seed), ("offset", offset)):
+        if int(v) != v or not 0 <= int(v) < 2 ** 64:
+            raise ValueError(f"{name} must be a whole number of 64 bits, got {v}")
+    e.seed, e.offset = int(seed), int(offset)
+    if rng is not None:
+        if rng.dtype != torch.int64 or rng.numel() != 2 or rng.device != dev:
+            raise ValueError("rng must be two int64 (seed, offset) on the tensors' device")
+        if int(seed) != 0:
+            raise ValueError("rng holds the seed: give one of the two")
+        e.seed_dev = _dev(rng, "rng")
+        e.offset_dev = e.seed_dev + 8
+    return e
+
+
+def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None, dev=None):
+    """Pointer and row pitch of a tensor seen as rows of its last dimension."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor (the library has no CPU path)")
+    if t.dim() < 1:
+        raise ValueError(f"{name} has no channels")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, the others are {dtype}: one dtype per call")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} {tuple(t.shape)} must be {tuple(shape)}")
+    if dev is not None and t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, the others on {dev}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the channels of a token must be contiguous")
+    pitch = after = None      # of the innermost dimension with more than one row; where the one outside it has to step
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if pitch is None:
+            pitch = st
+        elif st != after:
+            raise ValueError(f"{name}: its tokens are not rows with one distance")
+        after = st * n
+    if pitch is not None and pitch < t.shape[-1]:
+        raise ValueError(f"{name}: its tokens overlap (an expanded tensor?)")
+    return t.data_ptr(), (pitch if pitch is not None else 0)
+
+
+def _rows_of(t: torch.Tensor) -> int:
+    return t.numel() // t.shape[-1] if t.shape[-1] else 0
+
+
+def lbp_linear_workspace_bytes(rows: int, Cin: int, Cout: int, dtype_code: int) -> int:
+    return int(_lib().lbp_linear_workspace_bytes(rows, Cin, Cout, dtype_code))
+
+
+def lbp_linear(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, *, activation="none",
+               residual: torch.Tensor | None = None, p: float = 0.0, seed: int = 0, offset: int = 0,
+               rng: torch.Tensor | None = None, save_z: bool = False, out: torch.Tensor | None = None,
+               z: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """y = residual + drop(act(x W^T + bias)) for x (..., Cin), W (Cout, Cin): one call.
+
+    Returns y (..., Cout), with save_z (or a tensor `z` to write to) the pair (y, z) with
+    z = x W^T + bias, which lbp_linear_grad, lbp_project_grad and lbp_backward_act take.
+    Dropout with probability p draws from the counter-based generator of include/lbp.h at
+    (seed, offset), or at the two int64 of the CUDA tensor `rng` (offset is added to its second),
+    which the kernel reads, so that a captured graph draws new numbers when they have changed.
+    x, residual, out and z may be views whose tokens lie at one distance; out may be the residual."""
+    got = _native().linear_forward(x, W, bias, activation, residual, p, seed, offset, rng, save_z, out, z, ws)
+    if got is not None:
+        return _result(got, "lbp_linear")
+    if W.dim() != 2 or x.dim() < 1 or x.shape[-1] != W.shape[1]:
+        raise ValueError(f"x {tuple(x.shape)} does not match W {tuple(W.shape)}: (..., Cin) and (Cout, Cin)")
+    code = _dtype_code(x.dtype)
+    Cout, Cin = W.shape
+    shape = tuple(x.shape[:-1]) + (Cout,)
+    e = _epilogue(activation, p, seed, offset, rng, x.device)
+    pt = Pitches()
+    px, pt.x = _matrix(x, "x")
+    pw = _matrix(W, "W", x.dtype, None, x.device)[0]
+    if not W.is_contiguous():
+        raise ValueError("W must be contiguous")
+    pb = pr = None
+    if bias is not None:
+        pb = _matrix(bias, "bias", x.dtype, (Cout,), x.device)[0]
+    if residual is not None:
+        pr, pt.residual = _matrix(residual, "residual", x.dtype, shape, x.device)
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    py, pt.y = _matrix(out, "out", x.dtype, shape, x.device)
+    if z is None and save_z:
+        z = torch.empty(shape, dtype=x.dtype, device=x.device)
+    pz = None
+    if z is not None:
+        pz, pt.z = _matrix(z, "z", x.dtype, shape, x.device)
+    rows = _rows_of(x)
+    if ws is None:
+        n = lbp_linear_workspace_bytes(rows, Cin, Cout, code)
+        if n == 0:
+            raise ValueError("invalid layer for lbp_linear_workspace_bytes (channels must fill 16 bytes)")
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+    _check(_lib().lbp_linear(px, pw, pb, pr, py, pz, rows, Cin, Cout, code, C.byref(pt), C.byref(e),
+                             _dev(ws, "ws"), ws.numel() * ws.element_size(), _stream()), "lbp_linear")
+    return (out, z) if z is not None else out
+
+
+def lbp_linear_grad(g_y: torch.Tensor, z: torch.Tensor | None = None, *, activation="none", p: float = 0.0,
+                    seed: int = 0, offset: int = 0, rng: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """g_z = drop(g_y) act'(z): the gradient behind lbp_linear's epilogue (without an activation, that of
+    lbp_dropout).  z as lbp_linear has left it; p, seed, offset, rng as in the forward call.  out may be
+    g_y or z."""
+    got = _native().linear_grad(g_y, z, activation, p, seed, offset, rng, out)
+    if got is not None:
+        return _result(got, "lbp_linear_grad")
+    code = _dtype_code(g_y.dtype)
+    e = _epilogue(activation, p, seed, offset, rng, g_y.device)
+    pt = Pitches()
+    pg, pt.y = _matrix(g_y, "g_y")
+    pz = None
+    if z is not None:
+        pz, pt.z = _matrix(z, "z", g_y.dtype, g_y.shape, g_y.device)
+    elif e.act:
+        raise ValueError("an activation needs z")
+    if out is None:
+        out = torch.empty(g_y.shape, dtype=g_y.dtype, device=g_y.device)
+    po, pt.x = _matrix(out, "out", g_y.dtype, g_y.shape, g_y.device)
+    _check(_lib().lbp_linear_grad(pg, pz, po, _rows_of(g_y), g_y.shape[-1], code, C.byref(pt), C.byref(e), _stream()),
+           "lbp_linear_grad")
+    return out
+
+
+def lbp_dropout(x: torch.Tensor, p: float, *, seed: int = 0, offset: int = 0, rng: torch.Tensor | None = None,
+                residual: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y = residual + drop(x), with no mask in memory.  Its backward pass is lbp_dropout of the gradient at the
+    same seed and offset.  out may be x or the residual."""
+    got = _native().dropout(x, p, seed, offset, rng, residual, out)
+    if got is not None:
+        return _result(got, "lbp_dropout")
+    code = _dtype_code(x.dtype)
+    e = _epilogue(None, p, seed, offset, rng, x.device)
+    pt = Pitches()
+    px, pt.x = _matrix(x, "x")
+    pr = None
+    if residual is not None:
+        pr, pt.residual = _matrix(residual, "residual", x.dtype, x.shape, x.device)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    po, pt.y = _matrix(out, "out", x.dtype, x.shape, x.device)
+    _check(_lib().lbp_dropout(px, pr, po, _rows_of(x), x.shape[-1], code, C.byref(pt), C.byref(e), _stream()),
+           "lbp_dropout")
+    return out
+
+
+def lbp_project_grad_workspace_bytes(B: int, H: int, W: int, Cc: int, k: int, r: int, dtype_code: int) -> int:
+    return int(_lib().lbp_project_grad_workspace_bytes(B, H, W, Cc, k, r, dtype_code))
+
+
+def lbp_project_grad(g_y: torch.Tensor, z: torch.Tensor | None, k: int, bases, *, activation="none", p: float = 0.0,
+                     seed: int = 0, offset: int = 0, rng: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """lbp_project of g_z = drop(g_y) act'(z): (B,H,W,C) -> (B,ceil(H/k),ceil(W/k),r,C)."""
+    got = _native().project_grad(g_y, z, k, bases, activation, p, seed, offset, rng, out, ws)
+    if got is not None:
+        return _result(got, "lbp_project_grad")
+    if g_y.dim() != 4:
+        raise ValueError("g_y must be (B, H, W, C)")
+    code, dev, r = _dtype_code(g_y.dtype), g_y.device, len(bases)
+    B, H, W, Cc = g_y.shape
+    e = _epilogue(activation, p, seed, offset, rng, dev)
+    pg, v = _dev_view(g_y, "g_y")
+    pz = None
+    if z is not None:
+        pz, vz = _dev_view(z, "z")
+        if z.dtype != g_y.dtype or z.device != dev or z.shape != g_y.shape or vz != v:
+            raise ValueError("z must be laid out as g_y: one dtype, device, shape and strides")
+    elif e.act:
+        raise ValueError("an activation needs z")
+    shape = (B, -(-H // max(k, 1)), -(-W // max(k, 1)), r, Cc)
+    if out is None:
+        out = torch.empty(shape, dtype=g_y.dtype, device=dev)
+    elif tuple(out.shape) != shape or out.dtype != g_y.dtype or out.device != dev:
+        raise ValueError(f"out must be {shape} of g_y's dtype and device")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    if ws is None:
+        n = lbp_project_grad_workspace_bytes(B, H, W, Cc, k, r, code)
+        ws = torch.empty(max(n, lbp_status_bytes()), dtype=torch.uint8, device=dev)
+    view = View(*v)
+    _check(_lib().lbp_project_grad(pg, pz, _dev(out, "t_hat"), B, H, W, Cc, k, _bases(bases), r, code, C.byref(view),
+                                   C.byref(e), _dev(ws, "ws"), ws.numel(), _stream()), "lbp_project_grad")
+    return out
+
+
+def lbp_backward_act(x, g_y, z, W, k: int, bases, *, activation="none", p: float = 0.0, seed: int = 0,
+                     offset: int = 0, rng=None, x_hat=None, beta: float = 0.0, g_bias=None, x_extra=None,
+                     gy_extra=None, gx_extra=None, z_extra=None, first: int = 0, number=None, first_extra: int = 0,
+                     number_extra: int = 0, gw_dtype: torch.dtype = torch.float32, g_x=None, g_W=None, ws=None):
+    """lbp_backward_ex on g_z = drop(g_y) act'(z), the gradient behind lbp_linear's epilogue.  z and
+    z_extra are laid out as g_y and gy_extra.  `first`, `number` (image, row, token), `first_extra` and
+    `number_extra` number the elements for drop() as in the forward call (default: the dense grid
+    alone); for the tokens of a (B, n + H*W, C) sequence first = n*C, number = ((n + H*W)*C, W*C, C)."""
+    if (x is None) == (x_hat is None):
+        raise ValueError("give exactly one of x and x_hat")
+    if g_y.dim() != 4:
+        raise ValueError("g_y must be (B, H, W, Cout)")
+    B, H, Wd, Cout = g_y.shape
+    r = len(bases)
+    Cin = (x if x is not None else x_hat).shape[-1]
+    _check_layer_tensors(g_y, W, g_x, g_W, Cin, x=x, x_hat=x_hat, k=k, r=r)
+    e = _epilogue(activation, p, seed, offset, rng, g_y.device)
+    e.first = int(first)
+    if number is not None:
+        e.number = View(*[int(v) for v in number])
+    if g_x is None:
+        g_x = torch.empty((B, H, Wd, Cin), dtype=g_y.dtype, device=g_y.device)
+    if g_W is None:
+        if beta != 0.0:
+            raise ValueError("beta != 0 accumulates into g_W: pass it")
+        g_W = torch.empty((Cout, Cin), dtype=gw_dtype, device=g_y.device)
+    ex = _extras(g_y, Cin, beta, g_bias, x_extra, gy_extra, gx_extra)
+    px = None
+    if x is not None:
+        px, v = _dev_view(x, "x")
+        ex.x_view = View(*v)
+    pgy, gv = _dev_view(g_y, "g_y")
+    ex.gy_view = View(*gv)
+    pgx, v = _dev_view(g_x, "g_x")
+    ex.gx_view = View(*v)
+    grad = LayerGrad()
+    grad.epilogue, grad.first_extra, grad.number_extra = e, int(first_extra), int(number_extra)
+    if z is not None:
+        grad.z, zv = _dev_view(z, "z")
+        if z.dtype != g_y.dtype or z.device != g_y.device or z.shape != g_y.shape or zv != gv:
+            raise ValueError("z must be laid out as g_y: one dtype, device, shape and strides")
+    elif e.act:
+        raise ValueError("an activation needs z")
+    if z_extra is not None:
+        grad.z_extra, zp = _dev_rows(z_extra, "z_extra")
+        if gy_extra is None or z_extra.shape != gy_extra.shape or z_extra.dtype != g_y.dtype or \
+                z_extra.device != g_y.device or zp != ex.gy_extra_pitch:
+            raise ValueError("z_extra must be laid out as gy_extra")
+    lay = _layer(B, H, Wd, Cin, Cout, k, _dtype_code(g_y.dtype), _dtype_code(g_W.dtype))
+    if ws is None:
+        n = int(_lib().lbp_workspace_bytes_act(C.byref(lay), r, C.byref(ex), 1 if x_hat is not None else 0))
+        if n == 0:
+            raise ValueError("invalid layer, strides or extras for lbp_workspace_bytes_act")
+        ws = torch.empty(n, dtype=torch.uint8, device=g_y.device)
+    _check(_lib().lbp_backward_act(px, None if x_hat is None else _dev(x_hat, "x_hat"), pgy, _dev(W, "W"), pgx,
+                                   _dev(g_W, "g_W"), C.byref(lay), _bases(bases), r, C.byref(ex), C.byref(grad),
+                                   _dev(ws, "ws"), ws.numel(), _stream()), "lbp_backward_act")
     return g_x, g_W
 
 

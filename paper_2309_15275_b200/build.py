@@ -18,7 +18,8 @@ TORCH_STAMP = os.path.join(HERE, "_build", "torch_version")
 
 SOURCES = ["lbp_host.cpp", "lbp_api.cu", "wht_project.cu", "wht_expand.cu",
            "gemm_fp32.cu", "gemm_fp32_split.cu", "gemm_bf16.cu", "lbp_fused.cu", "lbp_static.cu",
-           "wht_spectrum.cu", "lbp_extras.cu", "lbp_fused_plan.cu", "wht_project_umma.cu"]
+           "wht_spectrum.cu", "lbp_extras.cu", "lbp_fused_plan.cu", "wht_project_umma.cu",
+           "layer_api.cu", "layer_pointwise.cu", "layer_linear.cu"]
 
 
 def _nvcc() -> str:
@@ -56,7 +57,7 @@ def _binding_command() -> list:
             "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(root, "include"),
             "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
             "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"),
-            BINDING_SOURCE, "-o", BINDING, "-L", libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch",
+            BINDING_SOURCE, "-o", BINDING, "-L", libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch",
             "-ltorch_python", "-ldl", f"-Wl,-rpath,{libs}"]
 
 

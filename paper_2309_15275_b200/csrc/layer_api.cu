@@ -1,0 +1,327 @@
+// C-ABI entry points of what a layer does around its product: checks, workspace layout
+// and the launches.
+#include <cmath>
+#include <initializer_list>
+
+#include "layer_math.cuh"
+
+namespace lbp {
+namespace layer {
+
+static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+static int elem_size(int dtype) { return dtype == LBP_BF16 ? 2 : 4; }
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+static const lbp_epilogue kNoEpilogue{};
+static const lbp_pitches kDense{};
+
+// The numbers of a call's elements are below 2^62, so that no sum here overflows.
+constexpr int64_t kMostElements = int64_t{1} << 62;
+
+static int check_rows(long long rows, int C, int dtype) {
+  if (dtype != LBP_F32 && dtype != LBP_BF16) return LBP_ERR_DTYPE;
+  if (rows < 0 || rows > (1ll << 40) || C <= 0) return LBP_ERR_SHAPE;
+  if ((static_cast<long long>(C) * elem_size(dtype)) % 16 != 0) return LBP_ERR_ALIGN;
+  return LBP_OK;
+}
+static int check_pitch(int64_t pitch, int C, int dtype) {
+  if (pitch == 0) return LBP_OK;
+  if (pitch < C || pitch >= (int64_t{1} << 40)) return LBP_ERR_SHAPE;   // (a tensor map's stride)
+  return (pitch * elem_size(dtype)) % 16 != 0 ? LBP_ERR_ALIGN : LBP_OK;
+}
+static bool in_quads(int64_t v, int dtype) { return v % (dtype == LBP_BF16 ? 8 : 4) == 0; }
+
+static int check_epilogue(const lbp_epilogue& e, int dtype) {
+  if (e.act < LBP_ACT_NONE || e.act > LBP_ACT_SILU || !(e.p >= 0.f && e.p <= 1.f)) return LBP_ERR_SHAPE;
+  if (e.first < 0 || e.first >= kMostElements) return LBP_ERR_SHAPE;
+  for (int64_t v : {e.number.image, e.number.row, e.number.token})
+    if (v < 0 || v >= (int64_t{1} << 50)) return LBP_ERR_SHAPE;
+  for (int64_t v : {e.first, e.number.image, e.number.row, e.number.token})
+    if (!in_quads(v, dtype)) return LBP_ERR_ALIGN;
+  if (((reinterpret_cast<uintptr_t>(e.seed_dev) | reinterpret_cast<uintptr_t>(e.offset_dev) |
+        reinterpret_cast<uintptr_t>(e.used)) & 7u) != 0)
+    return LBP_ERR_ALIGN;
+  return LBP_OK;
+}
+
+static Drop drop_of(const lbp_epilogue& e) {
+  // t = p 2^16, to the nearest
+  const long t = std::lround(static_cast<double>(e.p) * 65536.0);
+  Drop d{};
+  d.seed = e.seed;
+  d.offset = e.offset;
+  d.seed_dev = e.seed_dev;
+  d.offset_dev = e.offset_dev;
+  d.used = e.used;
+  d.on = t > 0;
+  d.above = static_cast<uint32_t>(static_cast<uint64_t>(t > 0 ? t : 1) * 65536u - 1u);
+  d.scale = t < 65536 ? static_cast<float>(65536.0 / static_cast<double>(65536 - t)) : 0.f;
+  return d;
+}
+
+// The bytes of `rows` rows at p.
+struct Range {
+  uintptr_t lo, hi;
+};
+static Range range(const void* p, long long rows, int64_t pitch, int C, int dtype) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  if (p == nullptr || rows == 0) return Range{0, 0};
+  return Range{lo, lo + (static_cast<uintptr_t>(rows - 1) * pitch + C) * elem_size(dtype)};
+}
+static bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+
+static lbp_view rows_at(int64_t pitch) { return lbp_view{pitch, 0, 0}; }
+
+// drop(a) act'(z) (+ residual) on rows, after its checks.
+static int run_rows(const void* a, const void* z, const void* residual, void* out, long long rows, int C, int dtype,
+                    int64_t pa, int64_t pz, int64_t pr, int64_t po, const lbp_epilogue& e, cudaStream_t st) {
+  PointCall c{};
+  c.a = a;
+  c.z = z;
+  c.residual = residual;
+  c.out = out;
+  c.rows = rows;
+  c.C = C;
+  c.HW = c.W = 1;
+  c.dtype = dtype;
+  c.act = e.act;
+  c.va = rows_at(pa ? pa : C);
+  c.vz = rows_at(pz ? pz : C);
+  c.vr = rows_at(pr ? pr : C);
+  c.vo = rows_at(po ? po : C);
+  c.number = rows_at(e.number.token ? e.number.token : C);
+  c.first = e.first;
+  c.drop = drop_of(e);
+  return launch_pointwise(c, st);
+}
+
+// Whether g_y and z of a call on rows are as they should be.
+static int check_pointwise(const void* a, const void* b, bool need_b, const void* out, long long rows, int C, int dtype,
+                           const lbp_pitches& p, int64_t pa, int64_t pb, int64_t po, const lbp_epilogue& e) {
+  if (int s = check_rows(rows, C, dtype)) return s;
+  if (int s = check_epilogue(e, dtype)) return s;
+  for (int64_t v : {p.x, p.residual, p.y, p.z})
+    if (int s = check_pitch(v, C, dtype)) return s;
+  if (rows == 0) return LBP_OK;
+  if (a == nullptr || out == nullptr || (need_b && b == nullptr)) return LBP_ERR_NULL;
+  if (!aligned16(a) || !aligned16(b) || !aligned16(out)) return LBP_ERR_ALIGN;
+  // in place, or apart
+  const Range ro = range(out, rows, po ? po : C, C, dtype);
+  const auto bad = [&](const void* q, int64_t pq) {
+    return overlap(ro, range(q, rows, pq ? pq : C, C, dtype)) && (q != out || (pq ? pq : C) != (po ? po : C));
+  };
+  return bad(a, pa) || bad(b, pb) ? LBP_ERR_OVERLAP : LBP_OK;
+}
+
+static int check_shape(int B, int H, int W, int C, int k, int dtype) {
+  if (int s = check_order(k)) return s;
+  if (B <= 0 || H <= 0 || W <= 0) return LBP_ERR_SHAPE;
+  return check_rows(static_cast<long long>(B) * H * W, C, dtype);
+}
+static int check_grid_view(const lbp_view& v, int C, int dtype) {
+  if (v.image == 0 && v.row == 0 && v.token == 0) return LBP_OK;
+  if (v.image <= 0 || v.row <= 0 || v.token < C) return LBP_ERR_SHAPE;
+  for (int64_t s : {v.image, v.row, v.token}) {
+    if (s >= (int64_t{1} << 40) / elem_size(dtype)) return LBP_ERR_SHAPE;
+    if ((s * elem_size(dtype)) % 16 != 0) return LBP_ERR_ALIGN;
+  }
+  return LBP_OK;
+}
+
+// g_z = drop(g_y) act'(z) of a token grid into a dense tensor.
+static int run_grid(const void* g_y, const void* z, void* g_z, int B, int H, int W, int C, int dtype,
+                    const lbp_view* view, const lbp_epilogue& e, cudaStream_t st) {
+  PointCall c{};
+  c.a = g_y;
+  c.z = z;
+  c.out = g_z;
+  c.rows = static_cast<long long>(B) * H * W;
+  c.C = C;
+  c.HW = H * W;
+  c.W = W;
+  c.dtype = dtype;
+  c.act = e.act;
+  c.va = c.vz = resolve_view(view, H, W, C);
+  c.vo = resolve_view(nullptr, H, W, C);
+  c.number = resolve_view(&e.number, H, W, C);
+  c.first = e.first;
+  c.drop = drop_of(e);
+  return launch_pointwise(c, st);
+}
+
+static size_t grid_bytes(long long tokens, int C, int dtype) {
+  return align_up(static_cast<size_t>(tokens) * C * elem_size(dtype), 1024);
+}
+
+// What lbp_backward_act hands on: the extras of the call on g_z, which lies dense.
+static lbp_extras with_dense_gradient(const lbp_extras* ex) {
+  lbp_extras d = ex != nullptr ? *ex : lbp_extras{};
+  d.gy_view = lbp_view{0, 0, 0};
+  d.gy_extra_pitch = 0;
+  return d;
+}
+static size_t inner_bytes(const lbp_layer* layer, int r, const lbp_extras* ex, bool x_hat) {
+  return (x_hat ? lbp_workspace_bytes_projected : lbp_workspace_bytes_ex)(layer, r, ex);
+}
+
+}  // namespace layer
+}  // namespace lbp
+
+using namespace lbp;
+using namespace lbp::layer;
+
+extern "C" {
+
+size_t lbp_linear_workspace_bytes(long long rows, int Cin, int Cout, int dtype) {
+  if (check_rows(rows, Cin, dtype) != LBP_OK || check_rows(rows, Cout, dtype) != LBP_OK) return 0;
+  return kStatusBytes;
+}
+
+int lbp_linear(const void* x, const void* W, const void* bias, const void* residual, void* y, void* z,
+               long long rows, int Cin, int Cout, int dtype, const lbp_pitches* pitch,
+               const lbp_epilogue* epilogue, void* ws, size_t ws_bytes, void* stream) {
+  const lbp_epilogue& e = epilogue != nullptr ? *epilogue : kNoEpilogue;
+  const lbp_pitches& p = pitch != nullptr ? *pitch : kDense;
+  if (int s = check_rows(rows, Cin, dtype)) return s;
+  if (int s = check_rows(rows, Cout, dtype)) return s;
+  if (int s = check_epilogue(e, dtype)) return s;
+  if (int s = check_pitch(p.x, Cin, dtype)) return s;
+  for (int64_t v : {p.residual, p.y, p.z})
+    if (int s = check_pitch(v, Cout, dtype)) return s;
+  if (rows == 0) return LBP_OK;
+  if (x == nullptr || W == nullptr || y == nullptr) return LBP_ERR_NULL;
+  for (const void* q : {x, W, bias, residual, static_cast<const void*>(y), static_cast<const void*>(z),
+                        static_cast<const void*>(ws)})
+    if (!aligned16(q)) return LBP_ERR_ALIGN;
+  LinearCall c{};
+  c.px = p.x ? p.x : Cin;
+  c.pr = p.residual ? p.residual : Cout;
+  c.py = p.y ? p.y : Cout;
+  c.pz = p.z ? p.z : Cout;
+  const Range out[2] = {range(y, rows, c.py, Cout, dtype), range(z, rows, c.pz, Cout, dtype)};
+  const Range in[4] = {range(x, rows, c.px, Cin, dtype), range(W, Cout, Cin, Cin, dtype), range(bias, 1, Cout, Cout, dtype),
+                       range(residual, rows, c.pr, Cout, dtype)};
+  const bool in_place = residual == y && c.pr == c.py;
+  for (int o = 0; o < 2; ++o)
+    for (int i = 0; i < 4; ++i)
+      if (overlap(out[o], in[i]) && !(o == 0 && i == 3 && in_place)) return LBP_ERR_OVERLAP;
+  if (overlap(out[0], out[1])) return LBP_ERR_OVERLAP;
+  const size_t need = lbp_linear_workspace_bytes(rows, Cin, Cout, dtype);
+  if (ws == nullptr || ws_bytes < need) return LBP_ERR_WORKSPACE;
+  const Range scratch{reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + need};
+  for (const Range& q : {out[0], out[1], in[0], in[1], in[2], in[3]})
+    if (overlap(scratch, q)) return LBP_ERR_OVERLAP;
+  if (int s = check_device_arch()) return s;
+  c.x = x;
+  c.W = W;
+  c.bias = bias;
+  c.residual = residual;
+  c.y = y;
+  c.z = z;
+  c.rows = rows;
+  c.Cin = Cin;
+  c.Cout = Cout;
+  c.dtype = dtype;
+  c.act = e.act;
+  c.first = e.first;
+  c.step = e.number.token ? e.number.token : Cout;
+  c.drop = drop_of(e);
+  c.status = static_cast<uint32_t*>(ws);
+  c.scratch = static_cast<uint8_t*>(ws) + kStatusBytes;
+  c.scratch_bytes = ws_bytes - kStatusBytes;
+  return launch_linear(c, static_cast<cudaStream_t>(stream));
+}
+
+int lbp_linear_grad(const void* g_y, const void* z, void* g_z, long long rows, int C, int dtype,
+                    const lbp_pitches* pitch, const lbp_epilogue* epilogue, void* stream) {
+  const lbp_epilogue& e = epilogue != nullptr ? *epilogue : kNoEpilogue;
+  const lbp_pitches& p = pitch != nullptr ? *pitch : kDense;
+  if (int s = check_pointwise(g_y, z, e.act != LBP_ACT_NONE, g_z, rows, C, dtype, p, p.y, p.z, p.x, e)) return s;
+  if (rows == 0) return LBP_OK;
+  if (int s = check_device_arch()) return s;
+  return run_rows(g_y, z, nullptr, g_z, rows, C, dtype, p.y, p.z, 0, p.x, e, static_cast<cudaStream_t>(stream));
+}
+
+int lbp_dropout(const void* x, const void* residual, void* y, long long rows, int C, int dtype,
+                const lbp_pitches* pitch, const lbp_epilogue* epilogue, void* stream) {
+  const lbp_epilogue& e = epilogue != nullptr ? *epilogue : kNoEpilogue;
+  const lbp_pitches& p = pitch != nullptr ? *pitch : kDense;
+  if (e.act != LBP_ACT_NONE) return LBP_ERR_SHAPE;
+  if (int s = check_pointwise(x, residual, false, y, rows, C, dtype, p, p.x, p.residual, p.y, e)) return s;
+  if (rows == 0) return LBP_OK;
+  if (int s = check_device_arch()) return s;
+  return run_rows(x, nullptr, residual, y, rows, C, dtype, p.x, 0, p.residual, p.y, e, static_cast<cudaStream_t>(stream));
+}
+
+size_t lbp_project_grad_workspace_bytes(int B, int H, int W, int C, int k, int r, int dtype) {
+  if (check_shape(B, H, W, C, k, dtype) != LBP_OK || r < 1 || r > k * k) return 0;
+  return 1024 + grid_bytes(static_cast<long long>(B) * H * W, C, dtype);
+}
+
+int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, int W, int C, int k,
+                     const lbp_basis* set, int r, int dtype, const lbp_view* view,
+                     const lbp_epilogue* epilogue, void* ws, size_t ws_bytes, void* stream) {
+  const lbp_epilogue& e = epilogue != nullptr ? *epilogue : kNoEpilogue;
+  if (g_y == nullptr || t_hat == nullptr || (z == nullptr && e.act != LBP_ACT_NONE)) return LBP_ERR_NULL;
+  if (int s = check_shape(B, H, W, C, k, dtype)) return s;
+  if (int s = check_epilogue(e, dtype)) return s;
+  if (view != nullptr)
+    if (int s = check_grid_view(*view, C, dtype)) return s;
+  BasisPlan plan;
+  if (int s = make_basis_plan(k, set, r, &plan)) return s;
+  if (!aligned16(g_y) || !aligned16(z) || !aligned16(t_hat) || !aligned16(ws)) return LBP_ERR_ALIGN;
+  if (ws == nullptr || ws_bytes < lbp_project_grad_workspace_bytes(B, H, W, C, k, r, dtype)) return LBP_ERR_WORKSPACE;
+  if (int s = check_device_arch()) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  void* const g_z = static_cast<uint8_t*>(ws) + 1024;
+  if (int s = run_grid(g_y, z, g_z, B, H, W, C, dtype, view, e, st)) return s;
+  return launch_project(g_z, t_hat, dtype, B, H, W, C, plan, static_cast<uint32_t*>(ws), st);
+}
+
+size_t lbp_workspace_bytes_act(const lbp_layer* layer, int r, const lbp_extras* ex, int x_hat) {
+  const lbp_extras d = with_dense_gradient(ex);
+  const size_t inner = inner_bytes(layer, r, &d, x_hat != 0);
+  if (inner == 0) return 0;
+  return align_up(inner, 1024) + grid_bytes(static_cast<long long>(layer->B) * layer->H * layer->W, layer->Cout, layer->dtype) +
+         grid_bytes(d.n_extra, layer->Cout, layer->dtype);
+}
+
+int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const void* W, void* g_x, void* g_W,
+                     const lbp_layer* layer, const lbp_basis* set, int r, const lbp_extras* ex,
+                     const lbp_layer_grad* grad, void* ws, size_t ws_bytes, void* stream) {
+  if (grad == nullptr || layer == nullptr || g_y == nullptr) return LBP_ERR_NULL;
+  const lbp_epilogue& e = grad->epilogue;
+  const bool has_act = e.act != LBP_ACT_NONE;
+  if (int s = check_epilogue(e, layer->dtype)) return s;
+  const int n_extra = ex != nullptr ? ex->n_extra : 0, dtype = layer->dtype, C = layer->Cout;
+  if (has_act && (grad->z == nullptr || (n_extra > 0 && grad->z_extra == nullptr))) return LBP_ERR_NULL;
+  if (!aligned16(grad->z) || !aligned16(grad->z_extra)) return LBP_ERR_ALIGN;
+  if (grad->first_extra < 0 || grad->first_extra >= kMostElements || grad->number_extra < 0 ||
+      grad->number_extra >= (int64_t{1} << 50))
+    return LBP_ERR_SHAPE;
+  if (!in_quads(grad->first_extra, dtype) || !in_quads(grad->number_extra, dtype)) return LBP_ERR_ALIGN;
+  // the call as it is, for what is wrong with it apart from the epilogue
+  if (int s = backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, true)) return s;
+  const size_t need = lbp_workspace_bytes_act(layer, r, ex, x_hat != nullptr);
+  if (need == 0 || ws_bytes < need) return LBP_ERR_WORKSPACE;
+  if (int s = check_device_arch()) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  lbp_extras d = with_dense_gradient(ex);
+  const size_t inner = align_up(inner_bytes(layer, r, &d, x_hat != nullptr), 1024);
+  uint8_t* const g_z = static_cast<uint8_t*>(ws) + inner;
+  if (int s = run_grid(g_y, grad->z, g_z, layer->B, layer->H, layer->W, C, dtype, ex != nullptr ? &ex->gy_view : nullptr, e, st))
+    return s;
+  if (n_extra > 0) {
+    lbp_epilogue ee = e;
+    ee.first = grad->first_extra;
+    ee.number = lbp_view{0, 0, grad->number_extra};
+    ee.used = nullptr;
+    uint8_t* const g_ze = g_z + grid_bytes(static_cast<long long>(layer->B) * layer->H * layer->W, C, dtype);
+    if (int s = run_rows(ex->gy_extra, grad->z_extra, nullptr, g_ze, n_extra, C, dtype, ex->gy_extra_pitch,
+                         ex->gy_extra_pitch, 0, 0, ee, st))
+      return s;
+    d.gy_extra = g_ze;
+  }
+  return backward_ex_call(x, x_hat, g_z, W, g_x, g_W, layer, set, r, &d, ws, inner, stream, false);
+}
+
+}  // extern "C"

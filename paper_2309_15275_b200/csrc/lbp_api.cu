@@ -668,6 +668,9 @@ size_t lbp_test_struct_size(int which) {
     case 1: return sizeof(lbp_extras);
     case 2: return sizeof(lbp_view);
     case 3: return sizeof(lbp_basis);
+    case 4: return sizeof(lbp_epilogue);
+    case 5: return sizeof(lbp_pitches);
+    case 6: return sizeof(lbp_layer_grad);
   }
   return 0;
 }
@@ -1086,6 +1089,30 @@ static int run_backward_ex(const void* x, const void* x_hat, const void* g_y, co
   return LBP_OK;
 }
 
+int backward_ex_call(const void* x, const void* x_hat, const void* g_y, const void* W, void* g_x, void* g_W,
+                     const lbp_layer* layer, const lbp_basis* set, int r, const lbp_extras* ex, void* ws,
+                     size_t ws_bytes, void* stream, bool check_only) {
+  if ((x == nullptr) == (x_hat == nullptr)) return LBP_ERR_NULL;   // exactly one of the two
+  const void* xin = x != nullptr ? x : x_hat;
+  BasisPlan plan;
+  Layout lay;
+  if (int e = validate_backward(xin, g_y, W, g_x, g_W, layer, set, r, ws, ws_bytes, &plan, &lay, x_hat != nullptr))
+    return e;
+  if (int e = check_extras(ex, layer)) return e;
+  // the K slices of the fp32 products make do with what there is behind the rest
+  const size_t need = total_with_extras(*layer, lay, r, ex);
+  if (ws_bytes < need) {
+    const size_t over = align_up(need - ws_bytes, 1024);
+    if (layer->dtype != LBP_F32 || over > lay.splitk_bytes) return LBP_ERR_WORKSPACE;
+    lay.splitk_bytes -= over;
+    lay.total -= over;
+  }
+  if (check_only) return LBP_OK;
+  if (int e = check_device_arch()) return e;
+  return run_backward_ex(x, x_hat, g_y, W, g_x, g_W, *layer, plan, lay, ex,
+                         static_cast<uint8_t*>(ws), static_cast<cudaStream_t>(stream));
+}
+
 }  // namespace lbp
 
 extern "C" {
@@ -1114,24 +1141,7 @@ size_t lbp_workspace_bytes_projected(const lbp_layer* layer, int r, const lbp_ex
 int lbp_backward_ex(const void* x, const void* x_hat, const void* g_y, const void* W, void* g_x,
                     void* g_W, const lbp_layer* layer, const lbp_basis* set, int r,
                     const lbp_extras* ex, void* ws, size_t ws_bytes, void* stream) {
-  if ((x == nullptr) == (x_hat == nullptr)) return LBP_ERR_NULL;   // exactly one of the two
-  const void* xin = x != nullptr ? x : x_hat;
-  BasisPlan plan;
-  Layout lay;
-  if (int e = validate_backward(xin, g_y, W, g_x, g_W, layer, set, r, ws, ws_bytes, &plan, &lay, x_hat != nullptr))
-    return e;
-  if (int e = check_extras(ex, layer)) return e;
-  // the K slices of the fp32 products make do with what there is behind the rest
-  const size_t need = total_with_extras(*layer, lay, r, ex);
-  if (ws_bytes < need) {
-    const size_t over = align_up(need - ws_bytes, 1024);
-    if (layer->dtype != LBP_F32 || over > lay.splitk_bytes) return LBP_ERR_WORKSPACE;
-    lay.splitk_bytes -= over;
-    lay.total -= over;
-  }
-  if (int e = check_device_arch()) return e;
-  return run_backward_ex(x, x_hat, g_y, W, g_x, g_W, *layer, plan, lay, ex,
-                         static_cast<uint8_t*>(ws), static_cast<cudaStream_t>(stream));
+  return backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, false);
 }
 
 int lbp_backward_projected(const void* x_hat, const void* g_y, const void* W, void* g_x, void* g_W,

@@ -268,4 +268,9 @@ int validate_backward_call(const void* x, const void* g_y, const void* W, const 
                            const void* g_W, const lbp_layer* layer, const lbp_basis* set, int r,
                            const void* ws, size_t ws_bytes);
 
+// lbp_backward_ex; check_only: its checks, and nothing is enqueued.
+int backward_ex_call(const void* x, const void* x_hat, const void* g_y, const void* W, void* g_x, void* g_W,
+                     const lbp_layer* layer, const lbp_basis* set, int r, const lbp_extras* ex, void* ws,
+                     size_t ws_bytes, void* stream, bool check_only);
+
 }  // namespace lbp

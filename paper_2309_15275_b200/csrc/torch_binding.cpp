@@ -13,6 +13,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/autocast_mode.h>
+#include <ATen/cuda/CUDAGeneratorImpl.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
@@ -23,6 +24,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
+#include <mutex>
 #include <optional>
 #include <string>
 #include <vector>
@@ -47,6 +49,14 @@ struct Library {
   decltype(&lbp_backward_ex) backward_ex;
   decltype(&lbp_backward_batch) backward_batch;
   decltype(&lbp_backward_fullrank) backward_fullrank;
+  decltype(&lbp_linear_workspace_bytes) linear_workspace_bytes;
+  decltype(&lbp_linear) linear;
+  decltype(&lbp_linear_grad) linear_grad;
+  decltype(&lbp_dropout) dropout;
+  decltype(&lbp_project_grad_workspace_bytes) project_grad_workspace_bytes;
+  decltype(&lbp_project_grad) project_grad;
+  decltype(&lbp_workspace_bytes_act) workspace_bytes_act;
+  decltype(&lbp_backward_act) backward_act;
 } lib;
 PyObject* error_type = nullptr;   // binding.LbpError
 
@@ -149,7 +159,7 @@ bool view_of(const Tensor& t, int dev, lbp_view* v) {
   const int64_t row = H > 1 ? t.stride(1) : W * tok;
   const int64_t img = B > 1 ? t.stride(0) : H * row;
   *v = lbp_view{img, row, tok};
-  return true;
+  return img != 0 || row != 0 || tok != 0;   // (an expanded tensor would read as dense)
 }
 // Row pitch of an (n, C) matrix (0: dense).
 bool rows_of(const Tensor& t, int dev, int64_t* pitch) {
@@ -158,7 +168,7 @@ bool rows_of(const Tensor& t, int dev, int64_t* pitch) {
   if (t.is_contiguous()) return true;
   if (t.size(1) > 1 && t.stride(1) != 1) return false;
   *pitch = t.size(0) > 1 ? t.stride(0) : 0;
-  return true;
+  return t.size(0) <= 1 || *pitch != 0;   // (an expanded tensor would read as dense)
 }
 
 Tensor bytes_on(const Tensor& like, size_t n) {
@@ -316,6 +326,7 @@ struct ExCall {
   Tensor x, x_hat, g_y, W, g_bias, x_extra, gy_extra, gx_extra, g_x, g_W, ws;
   double beta = 0.0;
   int k = 0, gw_code = LBP_F32;
+  const lbp_layer_grad* grad = nullptr;   // lbp_backward_act
 };
 // Returns the library's status, or -1 where a check does not hold (nothing done).
 int run_ex(ExCall* c, const lbp_basis* set, int r) {
@@ -359,11 +370,18 @@ int run_ex(ExCall* c, const lbp_basis* set, int r) {
       !view_of(c->g_x, dev, &ex.gx_view))
     return -1;
   if (!c->ws.defined()) {
-    const size_t bytes = (c->x_hat.defined() ? lib.workspace_bytes_projected : lib.workspace_bytes_ex)(&L, r, &ex);
+    const size_t bytes = c->grad != nullptr ? lib.workspace_bytes_act(&L, r, &ex, c->x_hat.defined() ? 1 : 0)
+                         : c->x_hat.defined() ? lib.workspace_bytes_projected(&L, r, &ex)
+                                              : lib.workspace_bytes_ex(&L, r, &ex);
     if (bytes == 0) return -1;
     c->ws = bytes_on(c->g_y, bytes);
   }
   if (!dense_on(c->ws, dev)) return -1;
+  if (c->grad != nullptr)
+    return lib.backward_act(c->x.defined() ? c->x.data_ptr() : nullptr,
+                            c->x_hat.defined() ? c->x_hat.data_ptr() : nullptr, c->g_y.data_ptr(), c->W.data_ptr(),
+                            c->g_x.data_ptr(), c->g_W.data_ptr(), &L, set, r, &ex, c->grad, c->ws.data_ptr(),
+                            c->ws.numel(), current_stream(dev));
   return lib.backward_ex(c->x.defined() ? c->x.data_ptr() : nullptr,
                          c->x_hat.defined() ? c->x_hat.data_ptr() : nullptr, c->g_y.data_ptr(), c->W.data_ptr(),
                          c->g_x.data_ptr(), c->g_W.data_ptr(), &L, set, r, &ex, c->ws.data_ptr(), c->ws.numel(),
@@ -561,6 +579,18 @@ bool makes_subclasses(PyTypeObject* type) {
   return !pybind11::getattr(reinterpret_cast<PyObject*>(type), "__torch_function__", off).is(off);
 }
 
+// y, as a subclass where one is among the n operands, as under torch's own functions.
+PyObject* wrap_like(const Tensor& y, PyObject* const* a, int n) {
+  PyObject* out = THPVariable_Wrap(y);
+  for (int i = 0; i < n && out != nullptr && THPVariable_CheckExact(out); ++i)
+    if (THPVariable_Check(a[i]) && !THPVariable_CheckExact(a[i]) && makes_subclasses(Py_TYPE(a[i]))) {
+      PyObject* as = PyObject_CallMethod(out, "as_subclass", "O", Py_TYPE(a[i]));
+      Py_DECREF(out);
+      out = as;
+    }
+  return out;
+}
+
 // linear(x, weight, bias | None, k, bases, save_projected, H, W) -> y
 PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -587,15 +617,446 @@ PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
                               static_cast<int64_t>(k), flat, projected, static_cast<int64_t>(H),
                               static_cast<int64_t>(W));
   }
-  PyObject* out = THPVariable_Wrap(y);
-  // a subclass among the operands makes the result one, as under torch's own functions
-  for (int i = 0; i < 3 && out != nullptr && THPVariable_CheckExact(out); ++i)
-    if (THPVariable_Check(a[i]) && !THPVariable_CheckExact(a[i]) && makes_subclasses(Py_TYPE(a[i]))) {
-      PyObject* as = PyObject_CallMethod(out, "as_subclass", "O", Py_TYPE(a[i]));
-      Py_DECREF(out);
-      out = as;
+  return wrap_like(y, a, 3);
+  END_HANDLE_TH_ERRORS
+}
+
+// ---- what a layer does around its product ----
+bool parse_act(PyObject* o, int32_t* act) {
+  static const char* const names[] = {"none", "relu", "gelu", "gelu_tanh", "silu"};
+  *act = LBP_ACT_NONE;
+  if (o == Py_None) return true;
+  if (!PyUnicode_Check(o)) return false;
+  for (int i = 0; i < 5; ++i)
+    if (PyUnicode_CompareWithASCIIString(o, names[i]) == 0) {
+      *act = i;
+      return true;
     }
-  return out;
+  return false;
+}
+bool parse_u64(PyObject* o, uint64_t* v) {
+  if (!PyLong_Check(o)) return false;
+  *v = PyLong_AsUnsignedLongLong(o);
+  if (PyErr_Occurred() == nullptr) return true;
+  PyErr_Clear();
+  return false;
+}
+// p, seed, offset, rng (the last an undefined tensor for None; it has to outlive the call)
+bool parse_drop(PyObject* const* a, lbp_epilogue* e, Tensor* rng) {
+  if (PyFloat_Check(a[0]))
+    e->p = static_cast<float>(PyFloat_AS_DOUBLE(a[0]));
+  else if (PyLong_CheckExact(a[0]))
+    e->p = static_cast<float>(PyLong_AsDouble(a[0]));
+  else
+    return false;
+  if (PyErr_Occurred() != nullptr) {
+    PyErr_Clear();
+    return false;
+  }
+  return e->p >= 0.f && e->p <= 1.f && parse_u64(a[1], &e->seed) && parse_u64(a[2], &e->offset) && parse_tensor(a[3], rng);
+}
+// The numbers' state in device memory, {seed, offset}.
+bool use_rng(const Tensor& rng, int dev, lbp_epilogue* e) {
+  if (!rng.defined()) return true;
+  if (rng.scalar_type() != at::kLong || rng.numel() != 2 || !dense_on(rng, dev) || e->seed != 0) return false;
+  e->seed_dev = static_cast<const uint64_t*>(rng.data_ptr());
+  e->offset_dev = e->seed_dev + 1;
+  return true;
+}
+// Rows of the last dimension at one distance (0: dense).
+bool matrix_of(const Tensor& t, int dev, int64_t* pitch) {
+  *pitch = 0;
+  if (!t.is_cuda() || t.get_device() != dev || t.dim() < 1) return false;
+  if (t.is_contiguous()) return true;
+  const int64_t last = t.dim() - 1, C = t.size(last);
+  if (C > 1 && t.stride(last) != 1) return false;
+  int64_t after = -1;
+  for (int64_t d = last - 1; d >= 0; --d) {
+    const int64_t n = t.size(d);
+    if (n == 1) continue;
+    if (after < 0)
+      *pitch = t.stride(d);
+    else if (t.stride(d) != after)
+      return false;
+    after = t.stride(d) * n;
+  }
+  return after < 0 || *pitch >= C;
+}
+// A matrix like another: its pitch, 0 for an undefined one.
+bool matrix_like(const Tensor& t, const Tensor& like, at::IntArrayRef shape, int dev, int64_t* pitch) {
+  *pitch = 0;
+  return !t.defined() || (t.scalar_type() == like.scalar_type() && t.sizes() == shape && matrix_of(t, dev, pitch));
+}
+void* data_or_null(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+bool on_current_device(const Tensor& t) { return t.defined() && t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+
+struct LinearArgs {
+  Tensor x, W, bias, residual, out, z, ws;
+  bool save_z = false;
+};
+// Returns the library's status, or -1 where a check does not hold (nothing done).
+int run_linear(LinearArgs* c, const lbp_epilogue& e) {
+  if (!on_current_device(c->x) || !c->W.defined() || c->W.dim() != 2 || c->x.dim() < 1) return -1;
+  const int dt = dtype_code(c->x.scalar_type()), dev = c->x.get_device();
+  const int64_t Cout = c->W.size(0), Cin = c->W.size(1);
+  if (dt < 0 || c->x.size(-1) != Cin || Cin < 1 || !int_size(Cin) || !int_size(Cout) ||
+      c->W.scalar_type() != c->x.scalar_type() || !dense_on(c->W, dev))
+    return -1;
+  if (c->bias.defined() && (c->bias.scalar_type() != c->x.scalar_type() || !has_shape(c->bias, {Cout}) || !dense_on(c->bias, dev)))
+    return -1;
+  c10::SmallVector<int64_t, 8> shape(c->x.sizes().begin(), c->x.sizes().end());
+  shape.back() = Cout;
+  const int64_t rows = c->x.numel() / Cin;
+  if (!c->out.defined()) c->out = at::empty(shape, c->x.options());
+  if (!c->z.defined() && c->save_z) c->z = at::empty(shape, c->x.options());
+  lbp_pitches p{};
+  if (!matrix_of(c->x, dev, &p.x) || !matrix_like(c->residual, c->x, shape, dev, &p.residual) ||
+      !matrix_like(c->out, c->x, shape, dev, &p.y) || !matrix_like(c->z, c->x, shape, dev, &p.z))
+    return -1;
+  if (!c->ws.defined()) {
+    const size_t bytes = lib.linear_workspace_bytes(rows, static_cast<int>(Cin), static_cast<int>(Cout), dt);
+    if (bytes == 0) return -1;
+    c->ws = bytes_on(c->x, bytes);
+  }
+  if (!dense_on(c->ws, dev)) return -1;
+  return lib.linear(c->x.data_ptr(), c->W.data_ptr(), data_or_null(c->bias), data_or_null(c->residual), c->out.data_ptr(),
+                    data_or_null(c->z), rows, static_cast<int>(Cin), static_cast<int>(Cout), dt, &p, &e, c->ws.data_ptr(),
+                    c->ws.nbytes(), current_stream(dev));
+}
+
+// linear_forward(x, W, bias, activation, residual, p, seed, offset, rng, save_z, out, z, ws)
+PyObject* py_linear_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  LinearArgs c;
+  lbp_epilogue e{};
+  Tensor rng;
+  if (n != 13 || !parse_tensor(a[0], &c.x) || !parse_tensor(a[1], &c.W) || !parse_tensor(a[2], &c.bias) ||
+      !parse_act(a[3], &e.act) || !parse_tensor(a[4], &c.residual) || !parse_drop(a + 5, &e, &rng) ||
+      !parse_tensor(a[10], &c.out) || !parse_tensor(a[11], &c.z) || !parse_tensor(a[12], &c.ws) ||
+      !on_current_device(c.x) || !use_rng(rng, c.x.get_device(), &e))
+    return not_handled();
+  c.save_z = a[9] == Py_True;
+  const int s = without_gil([&] { return run_linear(&c, e); });
+  if (s < 0) return not_handled();
+  return s != LBP_OK ? PyLong_FromLong(s) : c.z.defined() ? pair(c.out, c.z) : THPVariable_Wrap(c.out);
+  END_HANDLE_TH_ERRORS
+}
+
+// The pointwise calls: drop(a) with act'(b) or + b.  -1: not handled.
+int run_pointwise(const Tensor& a, const Tensor& b, Tensor* out, const lbp_epilogue& e, bool grad) {
+  if (!on_current_device(a) || a.dim() < 1) return -1;
+  const int dt = dtype_code(a.scalar_type()), dev = a.get_device();
+  const int64_t C = a.size(-1);
+  if (dt < 0 || C < 1 || !int_size(C)) return -1;
+  if (!out->defined()) *out = at::empty(a.sizes(), a.options());
+  int64_t pa, pb, po;
+  if (!matrix_of(a, dev, &pa) || !matrix_like(b, a, a.sizes(), dev, &pb) || !matrix_like(*out, a, a.sizes(), dev, &po))
+    return -1;
+  const int64_t rows = a.numel() / C;
+  if (grad) {
+    if (e.act != LBP_ACT_NONE && !b.defined()) return -1;
+    const lbp_pitches p{po, 0, pa, pb};
+    return lib.linear_grad(a.data_ptr(), data_or_null(b), out->data_ptr(), rows, static_cast<int>(C), dt, &p, &e,
+                           current_stream(dev));
+  }
+  const lbp_pitches p{pa, pb, po, 0};
+  return lib.dropout(a.data_ptr(), data_or_null(b), out->data_ptr(), rows, static_cast<int>(C), dt, &p, &e,
+                     current_stream(dev));
+}
+
+// linear_grad(g_y, z, activation, p, seed, offset, rng, out)
+PyObject* py_linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Tensor g_y, z, out, rng;
+  lbp_epilogue e{};
+  if (n != 8 || !parse_tensor(a[0], &g_y) || !parse_tensor(a[1], &z) || !parse_act(a[2], &e.act) ||
+      !parse_drop(a + 3, &e, &rng) || !parse_tensor(a[7], &out) || !on_current_device(g_y) ||
+      !use_rng(rng, g_y.get_device(), &e))
+    return not_handled();
+  const int s = without_gil([&] { return run_pointwise(g_y, z, &out, e, true); });
+  if (s < 0) return not_handled();
+  return s != LBP_OK ? PyLong_FromLong(s) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// dropout(x, p, seed, offset, rng, residual, out)
+PyObject* py_dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Tensor x, residual, out, rng;
+  lbp_epilogue e{};
+  if (n != 7 || !parse_tensor(a[0], &x) || !parse_drop(a + 1, &e, &rng) || !parse_tensor(a[5], &residual) ||
+      !parse_tensor(a[6], &out) || !on_current_device(x) || !use_rng(rng, x.get_device(), &e))
+    return not_handled();
+  const int s = without_gil([&] { return run_pointwise(x, residual, &out, e, false); });
+  if (s < 0) return not_handled();
+  return s != LBP_OK ? PyLong_FromLong(s) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// project_grad(g_y, z, k, bases, activation, p, seed, offset, rng, out, ws)
+PyObject* py_project_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Tensor g_y, z, rng, out, ws;
+  int k = 0;
+  Bases b;
+  lbp_epilogue e{};
+  lbp_view v, vz;
+  if (n != 11 || !parse_tensor(a[0], &g_y) || !parse_tensor(a[1], &z) || !parse_int(a[2], &k) || !parse_bases(a[3], &b) ||
+      !parse_act(a[4], &e.act) || !parse_drop(a + 5, &e, &rng) || !parse_tensor(a[9], &out) || !parse_tensor(a[10], &ws) ||
+      !on_current_device(g_y) || g_y.dim() != 4 || k < 1)
+    return not_handled();
+  const int dt = dtype_code(g_y.scalar_type()), dev = g_y.get_device();
+  if (dt < 0 || !view_of(g_y, dev, &v) || !use_rng(rng, dev, &e)) return not_handled();
+  for (int i = 0; i < 4; ++i)
+    if (!int_size(g_y.size(i))) return not_handled();
+  if (z.defined() ? z.scalar_type() != g_y.scalar_type() || z.sizes() != g_y.sizes() || !view_of(z, dev, &vz) ||
+                        vz.image != v.image || vz.row != v.row || vz.token != v.token
+                  : e.act != LBP_ACT_NONE)
+    return not_handled();
+  const int64_t shape[5] = {g_y.size(0), (g_y.size(1) + k - 1) / k, (g_y.size(2) + k - 1) / k, b.r, g_y.size(3)};
+  if (!out.defined())
+    out = at::empty(shape, g_y.options());
+  else if (!has_shape(out, shape) || out.scalar_type() != g_y.scalar_type() || !dense_on(out, dev))
+    return not_handled();
+  if (!ws.defined()) {
+    const size_t bytes = lib.project_grad_workspace_bytes(g_y.size(0), g_y.size(1), g_y.size(2), g_y.size(3), k, b.r, dt);
+    if (bytes == 0) return not_handled();
+    ws = bytes_on(g_y, bytes);
+  }
+  if (!dense_on(ws, dev)) return not_handled();
+  const int s = without_gil([&] {
+    return lib.project_grad(g_y.data_ptr(), data_or_null(z), out.data_ptr(), g_y.size(0), g_y.size(1), g_y.size(2),
+                            g_y.size(3), k, b.v, b.r, dt, &v, &e, ws.data_ptr(), ws.nbytes(), current_stream(dev));
+  });
+  return s != LBP_OK ? PyLong_FromLong(s) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// The state that one forward pass draws its numbers from: torch's generator of the device, so
+// that torch.manual_seed and a captured graph's replays have the meaning they have for torch's
+// own dropout.
+struct Drawn {
+  bool captured = false;
+  uint64_t seed = 0, offset = 0;
+  const uint64_t *seed_dev = nullptr, *offset_dev = nullptr;
+};
+Drawn draw_state(int dev) {
+  at::Generator gen = at::cuda::detail::getDefaultCUDAGenerator(static_cast<c10::DeviceIndex>(dev));
+  at::PhiloxCudaState s;
+  {
+    std::lock_guard<std::mutex> lock(gen.mutex());
+    s = at::check_generator<at::CUDAGeneratorImpl>(gen)->philox_cuda_state(4);
+  }
+  Drawn d;
+  d.captured = s.captured_;
+  if (s.captured_) {
+    d.seed_dev = reinterpret_cast<const uint64_t*>(s.seed_.ptr);
+    d.offset_dev = reinterpret_cast<const uint64_t*>(s.offset_.ptr);
+    d.offset = s.offset_intragraph_;
+  } else {
+    d.seed = s.seed_.val;
+    d.offset = s.offset_.val;
+  }
+  return d;
+}
+
+// y = residual + drop(act(x W^T + b)) with the gradient of the product by Algorithm 1: LinearFunction
+// with an epilogue.  The forward product is the library's too.
+struct LayerFunction : public torch::autograd::Function<LayerFunction> {
+  // What the forward pass computes; z is kept where a backward pass is to follow and needs it.
+  static Tensor compute(const Tensor& x, const Tensor& weight, const std::optional<Tensor>& bias,
+                        const std::optional<Tensor>& residual, int64_t act, double p, const Drawn& d, Tensor* z,
+                        Tensor* used) {
+    LinearArgs c;
+    lbp_epilogue e{};
+    e.act = static_cast<int32_t>(act);
+    e.p = static_cast<float>(p);
+    e.seed = d.seed;
+    e.offset = d.offset;
+    e.seed_dev = d.seed_dev;
+    e.offset_dev = d.offset_dev;
+    if (used != nullptr && d.captured) {
+      *used = at::empty({2}, x.options().dtype(at::kLong));
+      e.used = static_cast<uint64_t*>(used->data_ptr());
+    }
+    c.x = x.contiguous();
+    c.W = weight.contiguous();
+    if (bias.has_value()) c.bias = bias->contiguous();
+    if (residual.has_value()) c.residual = residual->contiguous();
+    c.save_z = z != nullptr && act != LBP_ACT_NONE;
+    const int s = run_linear(&c, e);
+    TORCH_CHECK_VALUE(s >= 0, "LbpLinear: x ", x.sizes(), " ", x.scalar_type(), ", weight ", weight.sizes(), " ",
+                      weight.scalar_type(), ", bias and residual do not fit together (CUDA tensors of one dtype, "
+                      "fp32 or bf16, on the current device; residual of the output's shape)");
+    if (s != LBP_OK) raise_status(s, "lbp_linear");
+    if (z != nullptr) *z = c.z;
+    return c.out;
+  }
+
+  static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& weight,
+                        const std::optional<Tensor>& bias, const std::optional<Tensor>& residual, int64_t k,
+                        const std::vector<int64_t>& bases, bool save_projected, int64_t H, int64_t W, int64_t act,
+                        double p) {
+    auto& saved = ctx->saved_data;
+    saved["k"] = k;
+    saved["bases"] = bases;
+    saved["bias"] = bias.has_value();
+    saved["residual"] = residual.has_value();
+    saved["H"] = H;
+    saved["W"] = W;
+    saved["act"] = act;
+    saved["p"] = p;
+    const Drawn d = p > 0.0 ? draw_state(x.get_device()) : Drawn{};
+    saved["seed"] = static_cast<int64_t>(d.seed);
+    saved["offset"] = static_cast<int64_t>(d.offset);
+    Tensor z, used, kept = x;
+    const Tensor y = compute(x, weight, bias, residual, act, p, d, &z, &used);
+    const bool projected = H <= 0 && save_projected;
+    if (projected) {
+      const Tensor xc = x.contiguous();
+      const std::vector<lbp_basis> set = LinearFunction::unpack(bases);
+      kept = at::empty({xc.size(0), (xc.size(1) + k - 1) / k, (xc.size(2) + k - 1) / k, static_cast<int64_t>(set.size()),
+                        xc.size(3)},
+                       xc.options());
+      Tensor ws = bytes_on(xc, lib.status_bytes());
+      const int s = lib.project(xc.data_ptr(), kept.data_ptr(), xc.size(0), xc.size(1), xc.size(2), xc.size(3),
+                                static_cast<int>(k), set.data(), static_cast<int>(set.size()),
+                                dtype_code(xc.scalar_type()), ws.data_ptr(), ws.numel(), current_stream(xc.get_device()));
+      if (s != LBP_OK) raise_status(s, "lbp_project");
+    }
+    saved["projected"] = projected;
+    ctx->save_for_backward({kept, weight, z, used});
+    return y;
+  }
+
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx,
+                                                 torch::autograd::variable_list grads) {
+    at::AutoGradMode no_grad(false);
+    auto& saved = ctx->saved_data;
+    const auto vars = ctx->get_saved_variables();
+    const std::vector<lbp_basis> set = LinearFunction::unpack(saved["bases"].toIntVector());
+    const int64_t H = saved["H"].toInt(), W = saved["W"].toInt();
+    TORCH_CHECK_VALUE(grads[0].is_cuda(), "g_y must be a CUDA tensor (the library has no CPU path)");
+    Tensor g_y = grads[0].contiguous();
+    Tensor z = vars[2];
+    const Tensor used = vars[3];
+    lbp_layer_grad g{};
+    g.epilogue.act = static_cast<int32_t>(saved["act"].toInt());
+    g.epilogue.p = static_cast<float>(saved["p"].toDouble());
+    g.epilogue.seed = static_cast<uint64_t>(saved["seed"].toInt());
+    g.epilogue.offset = static_cast<uint64_t>(saved["offset"].toInt());
+    if (used.defined()) {   // captured: what the forward pass has noted
+      g.epilogue.seed_dev = static_cast<const uint64_t*>(used.data_ptr());
+      g.epilogue.offset_dev = g.epilogue.seed_dev + 1;
+      g.epilogue.offset = 0;
+    }
+    ExCall c;
+    c.k = static_cast<int>(saved["k"].toInt());
+    c.W = vars[1].contiguous();
+    c.gw_code = dtype_code(c.W.scalar_type());
+    if (saved["bias"].toBool()) c.g_bias = at::empty({c.W.size(0)}, c.W.options());
+    Tensor g_x, cls;
+    int64_t n = 0;
+    const int64_t C = c.W.size(0);
+    if (H > 0) {
+      const Tensor x = vars[0].contiguous();
+      const int64_t B = x.size(0);
+      n = x.size(1) - H * W;
+      g_x = at::empty_like(x);
+      if (n > 1) {   // numbers of the extra tokens are no arithmetic series: the whole sequence at once
+        Tensor g_z;
+        const int s = run_pointwise(g_y, z, &g_z, g.epilogue, true);
+        TORCH_CHECK_VALUE(s >= 0, "LbpLinear: gradient and kept activation do not fit together");
+        if (s != LBP_OK) raise_status(s, "lbp_linear_grad");
+        g_y = g_z;
+        g = lbp_layer_grad{};
+        z = Tensor();
+      }
+      auto tokens = [&](const Tensor& t) {
+        return t.as_strided({B, H, W, t.size(2)}, {t.stride(0), W * t.size(2), t.size(2), 1},
+                            t.storage_offset() + n * t.size(2));
+      };
+      c.x = tokens(x);
+      c.g_y = tokens(g_y);
+      c.g_x = tokens(g_x);
+      if (z.defined()) g.z = tokens(z).data_ptr();
+      g.epilogue.first = n * C;
+      g.epilogue.number = lbp_view{(n + H * W) * C, W * C, C};
+      if (n == 1) {
+        c.x_extra = x.select(1, 0);
+        c.gy_extra = g_y.select(1, 0);
+        c.gx_extra = g_x.select(1, 0);
+        if (z.defined()) g.z_extra = z.data_ptr();
+        g.number_extra = (1 + H * W) * C;
+      } else if (n > 1) {
+        c.x_extra = x.narrow(1, 0, n).reshape({B * n, x.size(2)});
+        c.gy_extra = g_y.narrow(1, 0, n).reshape({B * n, g_y.size(2)});
+        c.gx_extra = cls = at::empty({B * n, x.size(2)}, x.options());
+      }
+    } else {
+      c.g_y = g_y;
+      if (z.defined()) g.z = z.data_ptr();
+      (saved["projected"].toBool() ? c.x_hat : c.x) = vars[0].contiguous();
+    }
+    c.grad = &g;
+    const int e = run_ex(&c, set.data(), static_cast<int>(set.size()));
+    TORCH_CHECK_VALUE(e >= 0, "LbpLinear: gradient, activation and weight do not fit together (shapes ", g_y.sizes(),
+                      ", ", vars[0].sizes(), ", ", c.W.sizes(), "; one dtype, the current device)");
+    if (e != LBP_OK) raise_status(e, "lbp_backward_act");
+    if (n > 1) g_x.narrow(1, 0, n).copy_(cls.view({g_x.size(0), n, g_x.size(2)}));
+    return {H > 0 ? g_x : c.g_x, c.g_W, c.g_bias, saved["residual"].toBool() ? grads[0] : Tensor(), Tensor(), Tensor(),
+            Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
+
+// layer(x, weight, bias | None, residual | None, k, bases, save_projected, H, W, activation, p) -> y
+PyObject* py_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Tensor x, weight, bias, residual;
+  int k = 0, H = 0, W = 0;
+  int32_t act = 0;
+  Bases b;
+  if (n != 11 || !parse_tensor(a[0], &x) || !parse_tensor(a[1], &weight) || !parse_tensor(a[2], &bias) ||
+      !parse_tensor(a[3], &residual) || !parse_int(a[4], &k) || k < 1 || !parse_bases(a[5], &b) || !parse_int(a[7], &H) ||
+      !parse_int(a[8], &W) || !parse_act(a[9], &act) || !PyFloat_Check(a[10]) || !x.defined() || !weight.defined() ||
+      (H > 0) != (W > 0)) {
+    PyErr_SetString(PyExc_ValueError,
+                    "layer: x, weight and residual are tensors, bases a list of (i, j) pairs, k and the grid positive");
+    return nullptr;
+  }
+  const double p = PyFloat_AS_DOUBLE(a[10]);
+  const bool projected = PyObject_IsTrue(a[6]) == 1;
+  std::vector<int64_t> flat(2 * b.r);
+  for (int q = 0; q < b.r; ++q) {
+    flat[2 * q] = b.v[q].i;
+    flat[2 * q + 1] = b.v[q].j;
+  }
+  Tensor y;
+  {
+    pybind11::gil_scoped_release no_gil;
+    TORCH_CHECK_VALUE(x.is_cuda(), "x must be a CUDA tensor (the library has no CPU path)");
+    TORCH_CHECK_VALUE(p >= 0.0 && p <= 1.0, "dropout is a probability, got ", p);
+    TORCH_CHECK_VALUE(H == 0 || (x.dim() == 3 && x.size(1) >= static_cast<int64_t>(H) * W),
+                      "with a grid, x must be (B, n + H*W, Cin)");
+    TORCH_CHECK_VALUE(H > 0 || x.dim() == 4, "x must be (B, H, W, Cin)");
+    // under autocast everything is of its type, as for torch's own product
+    if (at::autocast::is_autocast_enabled(at::kCUDA)) {
+      const at::ScalarType t = at::autocast::get_autocast_dtype(at::kCUDA);
+      for (Tensor* v : {&x, &weight, &bias, &residual})
+        if (v->defined() && v->is_floating_point()) *v = v->to(t);
+    }
+    const auto opt = [](const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; };
+    bool backward = false;
+    if (at::GradMode::is_enabled())
+      for (const Tensor* v : {&x, &weight, &bias, &residual}) backward |= v->defined() && v->requires_grad();
+    if (backward)
+      y = LayerFunction::apply(x, weight, opt(bias), opt(residual), static_cast<int64_t>(k), flat, projected,
+                               static_cast<int64_t>(H), static_cast<int64_t>(W), static_cast<int64_t>(act), p);
+    else
+      y = LayerFunction::compute(x, weight, opt(bias), opt(residual), act, p, p > 0.0 ? draw_state(x.get_device()) : Drawn{},
+                                 nullptr, nullptr);
+  }
+  return wrap_like(y, a, 4);
   END_HANDLE_TH_ERRORS
 }
 
@@ -645,7 +1106,14 @@ PyObject* py_load(PyObject*, PyObject* args) {
                   resolve(h, "lbp_project", &lib.project) && resolve(h, "lbp_spectrum", &lib.spectrum) &&
                   resolve(h, "lbp_backward", &lib.backward) && resolve(h, "lbp_backward_ex", &lib.backward_ex) &&
                   resolve(h, "lbp_backward_batch", &lib.backward_batch) &&
-                  resolve(h, "lbp_backward_fullrank", &lib.backward_fullrank);
+                  resolve(h, "lbp_backward_fullrank", &lib.backward_fullrank) &&
+                  resolve(h, "lbp_linear_workspace_bytes", &lib.linear_workspace_bytes) &&
+                  resolve(h, "lbp_linear", &lib.linear) && resolve(h, "lbp_linear_grad", &lib.linear_grad) &&
+                  resolve(h, "lbp_dropout", &lib.dropout) &&
+                  resolve(h, "lbp_project_grad_workspace_bytes", &lib.project_grad_workspace_bytes) &&
+                  resolve(h, "lbp_project_grad", &lib.project_grad) &&
+                  resolve(h, "lbp_workspace_bytes_act", &lib.workspace_bytes_act) &&
+                  resolve(h, "lbp_backward_act", &lib.backward_act);
   if (!ok) {
     PyErr_Format(PyExc_RuntimeError, "%s does not export what this binding calls", path);
     return nullptr;
@@ -665,6 +1133,11 @@ PyMethodDef methods[] = {{"load", py_load, METH_VARARGS, nullptr},
                          LBP_FAST("backward_ex", py_backward_ex),
                          LBP_FAST("backward_batch", py_backward_batch),
                          LBP_FAST("linear", py_linear),
+                         LBP_FAST("layer", py_layer),
+                         LBP_FAST("linear_forward", py_linear_forward),
+                         LBP_FAST("linear_grad", py_linear_grad),
+                         LBP_FAST("dropout", py_dropout),
+                         LBP_FAST("project_grad", py_project_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lbp_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
