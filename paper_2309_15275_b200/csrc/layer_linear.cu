@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) linear_tile_kernel(const __grid_constant_
   }
 }
 
-int launch_linear(const LinearCall& c, cudaStream_t stream) {
+static int launch_tile(const LinearCall& c, cudaStream_t stream) {
   const long long tiles = (c.rows + kTile - 1) / kTile;
   return with_act(c.act, [&](auto a) -> int {
     constexpr int ACT = decltype(a)::value;
@@ -75,6 +75,24 @@ int launch_linear(const LinearCall& c, cudaStream_t stream) {
     LBP_CUDA_TRY(cudaGetLastError());
     return LBP_OK;
   });
+}
+
+int launch_linear(const LinearCall& c, cudaStream_t stream) {
+  // coordinates of a tensor map are 32 bits wide
+  constexpr long long kMostRows = 1ll << 30;
+  LinearCall part = c;
+  const int es = c.dtype == LBP_BF16 ? 2 : 4;
+  for (long long at = 0; at < c.rows; at += kMostRows) {
+    auto from = [&](const void* q, int64_t pitch) { return q == nullptr ? nullptr : static_cast<const uint8_t*>(q) + at * pitch * es; };
+    part.rows = c.rows - at < kMostRows ? c.rows - at : kMostRows;
+    part.x = from(c.x, c.px);
+    part.residual = from(c.residual, c.pr);
+    part.y = const_cast<uint8_t*>(from(c.y, c.py));
+    part.z = const_cast<uint8_t*>(from(c.z, c.pz));
+    part.first = c.first + at * c.step;
+    if (int e = c.dtype == LBP_BF16 ? launch_linear_umma(part, stream) : launch_tile(part, stream)) return e;
+  }
+  return LBP_OK;
 }
 
 }  // namespace layer

@@ -1,0 +1,425 @@
+// y = residual + drop(act(x W^T + b)) for bf16 data on the tcgen05 tensor cores, the whole epilogue
+// behind the accumulator.
+//
+// A tile is 128 tokens by BN output channels; both operands are K-major as they lie (x by tokens, W by
+// output channels).  On CTA pairs (cta_group::2) a tile is 256 tokens, and each CTA fetches its own 128
+// tokens and half of W's rows.  Persistent, two accumulators in TMEM, so that the epilogue of a tile runs
+// under the products of the next.  Tiles go to the units round robin, a token tile's columns
+// next to one another, so that x comes from HBM once and W stays in L2.
+//
+// Warps: 0 TMA loads, 1 tcgen05, 2-9 the epilogue, two to each quarter of the accumulator's lanes, which
+// take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels: the
+// residual comes by TMA into a buffer of the warp's, a thread has a token (its channels lie
+// together, so that one Philox call serves eight of them), y goes back over the residual in shared memory
+// and out by TMA, z beside it.  The TMA clips what hangs over the last token and channel.
+#include "layer_math.cuh"
+#include "ptx_sm100.cuh"
+
+namespace lbp {
+namespace layer {
+
+namespace {
+
+constexpr int kBM = 128, kBK = 64;
+constexpr int kABytes = kBM * kBK * 2;
+constexpr int kEpilogueWarps = 8;
+constexpr int kThreads = (2 + kEpilogueWarps) * 32;
+constexpr int kBoxBytes = 32 * 64 * 2;                       // 32 tokens x 64 channels
+constexpr int kBufBytes = kEpilogueWarps * 2 * kBoxBytes;    // two a warp
+constexpr int kMaxStages = 8;
+constexpr int kBarBytes = 256;
+constexpr int kSmemMax = 227 * 1024;
+constexpr uint32_t kTmemCols = 512, kSlotCols = 256;
+constexpr uint32_t kSite = 8u << 16;
+
+struct Params {
+  const __nv_bfloat16* bias;
+  long long rows;
+  int32_t Cout, BN, num_kb, tiles_n, tiles, stages, stage_bytes;
+  int32_t residual, keep_z, test_stall;
+  int64_t first, step;
+  Drop drop;
+  uint32_t* status;
+};
+struct Maps {
+  CUtensorMap x, W, residual, y, z;
+};
+
+__device__ __forceinline__ void store_2d(const CUtensorMap* m, const void* src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(m)),
+               "r"(ptx::smem_u32(src)), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+template <int ACT, bool DROP, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_umma_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
+  constexpr int kCtas = PAIR ? 2 : 1;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* const bufs = smem + p.stages * p.stage_bytes;
+  uint64_t* const full = reinterpret_cast<uint64_t*>(bufs + kBufBytes);   // [kMaxStages]
+  uint64_t* const empty = full + kMaxStages;
+  uint64_t* const acc_full = empty + kMaxStages;    // [2]
+  uint64_t* const acc_empty = acc_full + 2;         // [2], the leader's are used
+  uint64_t* const arrived = acc_empty + 2;          // [kEpilogueWarps]: a warp's residual
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(arrived + kEpilogueWarps);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = PAIR ? static_cast<int>(ptx::cluster_ctarank()) : 0;
+  const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMaxStages; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      ptx::mbar_init(&acc_full[s], 1);
+      ptx::mbar_init(&acc_empty[s], kCtas * kEpilogueWarps);
+    }
+    for (int s = 0; s < kEpilogueWarps; ++s) ptx::mbar_init(&arrived[s], 1);
+    ptx::mbar_fence_init();
+    *abort_flag = 0;
+    ptx::prefetch_tensormap(&tm.x);
+    ptx::prefetch_tensormap(&tm.W);
+  }
+  if (warp == 1) {
+    if constexpr (PAIR) {
+      ptx::tmem_alloc_pair(tmem_slot, kTmemCols);
+      ptx::tmem_relinquish_pair();
+    } else {
+      ptx::tmem_alloc(tmem_slot, kTmemCols);
+      ptx::tmem_relinquish();
+    }
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if constexpr (PAIR) ptx::cluster_sync_all();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  // nothing is read or written before the kernel ahead has completed
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp == 0) {
+    // =========================== loads ===========================
+    if (ptx::elect_one()) {
+      asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+      const uint64_t keep = ptx::l2_policy_evict_last();
+      const int part = p.BN / kCtas;   // W's rows of this CTA
+      const uint32_t tx = static_cast<uint32_t>(kCtas * (kABytes + part * kBK * 2));
+      int s = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = unit; t < p.tiles && ok && !p.test_stall; t += units) {
+        const int m = t / p.tiles_n;
+        const int row = (m * kCtas + rank) * kBM, col = (t - m * p.tiles_n) * p.BN + rank * part;
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          if (!ptx::mbar_wait(&empty[s], phase ^ 1u, p.status, kSite | 1u)) {
+            ok = false;
+            break;
+          }
+          uint8_t* const sa = smem + s * p.stage_bytes;
+          if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);   // boxes count in full, also where they hang over
+          if constexpr (PAIR) {
+            const uint32_t bar = ptx::map_to_rank(ptx::smem_u32(&full[s]), 0);
+            ptx::tma_load_2d_pair(sa, &tm.x, bar, kb * kBK, row, keep);
+            ptx::tma_load_2d_pair(sa + kABytes, &tm.W, bar, kb * kBK, col, keep);
+          } else {
+            ptx::tma_load_2d_hint(sa, &tm.x, &full[s], kb * kBK, row, keep);
+            ptx::tma_load_2d_hint(sa + kABytes, &tm.W, &full[s], kb * kBK, col, keep);
+          }
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (warp == 1) {
+    // =========================== tcgen05 (leader only) ===========================
+    if (rank == 0 && ptx::elect_one()) {
+      const uint32_t idesc = ptx::idesc_bf16(kCtas * kBM, p.BN, false, false);
+      auto commit = [](uint64_t* bar) {
+        if constexpr (PAIR)
+          ptx::mma_commit_pair(bar);
+        else
+          ptx::mma_commit(bar);
+      };
+      int s = 0, n = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = unit; t < p.tiles && ok; t += units, ++n) {
+        const uint32_t d = tmem_base + (n & 1) * kSlotCols;
+        if (!ptx::mbar_wait(&acc_empty[n & 1], ((n >> 1) + 1) & 1u, p.status, kSite | 2u)) {
+          ok = false;
+          break;
+        }
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          if (!ptx::mbar_wait(&full[s], phase, p.status, kSite | 3u)) {
+            ok = false;
+            break;
+          }
+          ptx::tc_fence_after_sync();
+          const uint32_t sa = ptx::smem_u32(smem + s * p.stage_bytes), sb = sa + kABytes;
+#pragma unroll
+          for (int kk = 0; kk < kBK / 16; ++kk) {
+            const uint64_t da = ptx::smem_desc_sw128(sa + kk * 32, 16, 1024), db = ptx::smem_desc_sw128(sb + kk * 32, 16, 1024);
+            const uint32_t add = (kb == 0 && kk == 0) ? 0u : 1u;
+            if constexpr (PAIR)
+              ptx::mma_bf16_ss_pair(d, da, db, idesc, add);
+            else
+              ptx::mma_bf16_ss(d, da, db, idesc, add);
+          }
+          commit(&empty[s]);
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ok) commit(&acc_full[n & 1]);
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else {
+    // =========================== epilogue ===========================
+    const int e = warp - 2, sub = e >> 2, quarter = warp & 3;
+    uint8_t* const mine = bufs + e * 2 * kBoxBytes;
+    const Stream stream = DROP ? open_stream(p.drop) : Stream{};
+    if (blockIdx.x == 0 && warp == 2 && lane == 0) note_used(p.drop);
+    uint32_t uses = 0;   // residuals fetched
+    bool ok = true;
+    int n = 0;
+    const int chunks = p.BN / 64;
+    for (int t = unit; t < p.tiles && ok; t += units, ++n) {
+      const int m = t / p.tiles_n;
+      const long long row0 = static_cast<long long>(m * kCtas + rank) * kBM + quarter * 32;
+      const int col0 = (t - m * p.tiles_n) * p.BN;
+      const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols;
+      bool waited = false;
+      int last = -1;   // this warp's last chunk of the tile
+      for (int c = sub; c < chunks; c += 2) last = c;
+      for (int c = sub; c < chunks; c += 2) {
+        const int col = col0 + c * 64;
+        const bool any = row0 < p.rows && col < p.Cout;
+        uint8_t* const ybuf = mine + ((uses & 1u) && !p.keep_z ? kBoxBytes : 0);
+        if (any) {
+          if (lane == 0) {
+            bulk_wait_read();   // the buffers are free
+            if (p.residual) {
+              ptx::mbar_expect_tx(&arrived[e], kBoxBytes);
+              ptx::tma_load_2d(ybuf, &tm.residual, &arrived[e], col, static_cast<int32_t>(row0));
+            }
+          }
+          __syncwarp();
+        }
+        if (!waited) {
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u));
+          waited = true;
+          ptx::tc_fence_after_sync();
+        }
+        if (p.residual && any) ok &= __all_sync(0xffffffffu, ptx::mbar_wait(&arrived[e], uses & 1u, p.status, kSite | 5u));
+        if (!ok) break;
+        const uint64_t number = static_cast<uint64_t>(p.first + (row0 + lane) * p.step + col);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          uint32_t a[32];
+          ptx::tmem_ld_32x32(acc + c * 64 + h * 32, a);
+          ptx::tmem_ld_wait();
+          if (h == 1 && c == last) {   // the accumulator has been read
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+              if constexpr (PAIR)
+                ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
+              else
+                ptx::mbar_arrive(&acc_empty[n & 1]);
+            }
+          }
+          if (!any) continue;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {   // eight channels at a time
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(a[g * 8 + j]);
+            const int ch = col + h * 32 + g * 8;
+            if (p.bias != nullptr) {
+              uint4 w = make_uint4(0u, 0u, 0u, 0u);
+              if (ch < p.Cout) w = __ldg(reinterpret_cast<const uint4*>(p.bias + ch));
+              float b[8];
+              Vec<__nv_bfloat16>::unpack(w, b);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] += b[j];
+            }
+            const int at = lane * 128 + (((h * 4 + g) ^ (lane & 7)) << 4);
+            if (p.keep_z) *reinterpret_cast<uint4*>(mine + kBoxBytes + at) = Vec<__nv_bfloat16>::pack(v);
+            if constexpr (ACT != LBP_ACT_NONE) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = act<ACT, true>(v[j]);
+            }
+            if constexpr (DROP) drop(v, number + h * 32 + g * 8, stream, p.drop);
+            if (p.residual) {
+              float r[8];
+              Vec<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(ybuf + at), r);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] += r[j];
+            }
+            *reinterpret_cast<uint4*>(ybuf + at) = Vec<__nv_bfloat16>::pack(v);
+          }
+        }
+        if (any) {
+          ptx::fence_proxy_async_smem();   // the stores read through the async proxy
+          __syncwarp();
+          if (lane == 0) {
+            store_2d(&tm.y, ybuf, col, static_cast<int32_t>(row0));
+            if (p.keep_z) store_2d(&tm.z, mine + kBoxBytes, col, static_cast<int32_t>(row0));
+            bulk_commit();
+          }
+          ++uses;
+        }
+      }
+      if (last < 0) {   // a tile of one chunk: nothing of it is this warp's
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 6u));
+        if (lane == 0 && ok) {
+          if constexpr (PAIR)
+            ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
+          else
+            ptx::mbar_arrive(&acc_empty[n & 1]);
+        }
+      }
+      if (*abort_flag != 0) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+    }
+    if (!ok && lane == 0) *abort_flag = 1;
+    if (lane == 0) bulk_wait_all();
+  }
+
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if constexpr (PAIR) ptx::cluster_sync_all();   // neither CTA leaves while the other may still touch its memory
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    if constexpr (PAIR)
+      ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+    else
+      ptx::tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// How a product is cut.
+struct Plan {
+  bool pair;
+  int BN;
+};
+
+Plan choose_plan(const LinearCall& c, int sms) {
+  const int num_kb = (c.Cin + kBK - 1) / kBK;
+  Plan best{false, 64};
+  double least = -1.0;
+  for (int pair = 0; pair < 2; ++pair) {
+    if (pair && (c.rows <= kBM || sms < 2)) continue;
+    const int bm = pair ? 2 * kBM : kBM, units = pair ? sms / 2 : sms;
+    for (int bn = 64; bn <= 256; bn += 64) {
+      if (bn > 64 && bn - 64 >= c.Cout) continue;   // wider than the matrix
+      const long long tiles = ((c.rows + bm - 1) / bm) * ((c.Cout + bn - 1) / bn);
+      const double rounds = static_cast<double>((tiles + units - 1) / units);
+      // cycles of an SM: a k-block's products and operands (60 bytes a cycle), an element's epilogue
+      const double mma = 2.0 * bn, load = (kABytes + (pair ? bn / 2 : bn) * kBK * 2) / 60.0;
+      const double main = num_kb * (mma > load ? mma : load) + 200.0;
+      double per = 10.0;
+      if (c.act != LBP_ACT_NONE) per += 16.0;
+      if (c.drop.on) per += 12.0;
+      const double epi = bn * per + 500.0;
+      const double cost = rounds * (main > epi ? main : epi) + (main > epi ? epi : main) + 1500.0;
+      if (least < 0.0 || cost < least) {
+        least = cost;
+        best = Plan{pair != 0, bn};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace
+
+static thread_local bool g_test_stall = false;
+
+int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
+  int dev = 0, sms = 0;
+  LBP_CUDA_TRY(cudaGetDevice(&dev));
+  LBP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const Plan plan = choose_plan(c, sms);
+  const int ctas = plan.pair ? 2 : 1, part = plan.BN / ctas;
+  Params p{};
+  p.bias = static_cast<const __nv_bfloat16*>(c.bias);
+  p.rows = c.rows;
+  p.Cout = c.Cout;
+  p.BN = plan.BN;
+  p.num_kb = (c.Cin + kBK - 1) / kBK;
+  p.tiles_n = (c.Cout + plan.BN - 1) / plan.BN;
+  const long long tiles = ((c.rows + ctas * kBM - 1) / (ctas * kBM)) * p.tiles_n;
+  if (tiles >= (1ll << 31)) return LBP_ERR_SHAPE;
+  p.tiles = static_cast<int32_t>(tiles);
+  p.stage_bytes = kABytes + part * kBK * 2;
+  const int room = kSmemMax - 1024 - kBarBytes - kBufBytes;
+  p.stages = room / p.stage_bytes < kMaxStages ? room / p.stage_bytes : kMaxStages;
+  p.residual = c.residual != nullptr;
+  p.keep_z = c.z != nullptr;
+  p.test_stall = g_test_stall ? 1 : 0;
+  p.first = c.first;
+  p.step = c.step;
+  p.drop = c.drop;
+  p.status = c.status;
+  Maps tm;
+  if (int e = encode_matrix_tensor_map(&tm.x, c.x, c.rows, c.Cin, kBM, c.px)) return e;
+  if (int e = encode_matrix_tensor_map(&tm.W, c.W, c.Cout, c.Cin, part)) return e;
+  if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py)) return e;
+  tm.residual = tm.z = tm.y;
+  if (c.residual != nullptr)
+    if (int e = encode_matrix_tensor_map(&tm.residual, c.residual, c.rows, c.Cout, 32, c.pr)) return e;
+  if (c.z != nullptr)
+    if (int e = encode_matrix_tensor_map(&tm.z, c.z, c.rows, c.Cout, 32, c.pz)) return e;
+
+  const int units = plan.pair ? sms / 2 : sms;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas * (tiles < units ? tiles : units)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = 1024 + p.stages * p.stage_bytes + kBufBytes + kBarBytes;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = plan.pair ? 2 : 1;
+  return with_act(c.act, [&](auto a) -> int {
+    constexpr int ACT = decltype(a)::value;
+    auto launch = [&](auto kern, PerDevice& configured) -> int {
+      if (int e = allow_dynamic_smem(configured, reinterpret_cast<const void*>(kern), kSmemMax)) return e;
+      LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, tm, p));
+      count_launch();
+      return LBP_OK;
+    };
+    static PerDevice configured[4];
+    if (plan.pair)
+      return c.drop.on ? launch(linear_umma_kernel<ACT, true, true>, configured[3])
+                       : launch(linear_umma_kernel<ACT, false, true>, configured[2]);
+    return c.drop.on ? launch(linear_umma_kernel<ACT, true, false>, configured[1])
+                     : launch(linear_umma_kernel<ACT, false, false>, configured[0]);
+  });
+}
+
+}  // namespace layer
+
+void set_test_stall_linear(bool on) { layer::g_test_stall = on; }
+
+}  // namespace lbp

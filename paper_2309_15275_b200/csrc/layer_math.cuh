@@ -247,6 +247,7 @@ struct LinearCall {
   size_t scratch_bytes;
 };
 int launch_linear(const LinearCall& c, cudaStream_t stream);
+int launch_linear_umma(const LinearCall& c, cudaStream_t stream);   // bf16
 
 // out = residual + drop(a) act'(z) on the tokens of a grid (rows: H = W = 1)
 struct PointCall {

@@ -556,3 +556,21 @@ def test_tensors_of_another_device_are_refused(dev):
     for call in (lambda: lbp.lbp_linear(x, W, b), lambda: lbp.lbp_dropout(x, 0.5), lambda: lbp.lbp_linear_grad(x)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("rows,Cin,Cout", [(100, 128, 192), (1000, 128, 64), (1000, 192, 512)])
+def test_expired_wait_is_reported_and_the_next_call_is_clean(dev, rows, Cin, Cout):
+    """No load is issued (one CTA a tile, and pairs): the call reports it, and the next one on the same workspace is right."""
+    x, W, b = _inputs(rows, Cin, Cout, torch.bfloat16)
+    res = _normal((rows, Cout), 1.0, torch.bfloat16, 8)
+    ws = torch.zeros(lbp.lbp_linear_workspace_bytes(rows, Cin, Cout, lbp.LBP_BF16), dtype=torch.uint8, device=dev)
+    lbp.lbp_test_stall_products(True, linear=True)
+    try:
+        lbp.lbp_linear(x, W, b, residual=res, ws=ws)
+    finally:
+        lbp.lbp_test_stall_products(False)
+    assert lbp.lbp_poll_status(ws) == 10
+    assert lbp.lbp_poll_status(ws) == 0
+    y = lbp.lbp_linear(x, W, b, residual=res, ws=ws)
+    assert lbp.lbp_poll_status(ws) == 0
+    _check_linear(torch.bfloat16, y, None, _want_linear(x, W, b, "none", res, 0.0, 0, 0), 0.0)
