@@ -52,12 +52,14 @@ __global__ void __launch_bounds__(256) linear_tile_kernel(const __grid_constant_
       if (p.z != nullptr) static_cast<T*>(p.z)[row * p.pz + c + j] = static_cast<T>(v[j]);
       v[j] = act<ACT, V::kFast>(v[j]);
     }
-    if (p.drop.on) drop(v, p.first + row * p.step + c, s, p.drop);
+    float out[4] = {};
+    if (p.residual != nullptr) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (p.residual != nullptr) v[j] += static_cast<float>(static_cast<const T*>(p.residual)[row * p.pr + c + j]);
-      static_cast<T*>(p.y)[row * p.py + c + j] = static_cast<T>(v[j]);
+      for (int j = 0; j < 4; ++j) out[j] = static_cast<float>(static_cast<const T*>(p.residual)[row * p.pr + c + j]);
     }
+    add_dropped(out, v, p.first + row * p.step + c, s, p.drop);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) static_cast<T*>(p.y)[row * p.py + c + j] = static_cast<T>(out[j]);
   }
 }
 

@@ -7,11 +7,11 @@
 // under the products of the next.  Tiles go to the units round robin, a token tile's columns
 // next to one another, so that x comes from HBM once and W stays in L2.
 //
-// Warps: 0 TMA loads, 1 tcgen05, 2-9 the epilogue, two to each quarter of the accumulator's lanes, which
+// Warps: 0 TMA loads, 1 tcgen05, 2-17 the epilogue, four to each quarter of the accumulator's lanes, which
 // take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels: the
 // residual comes by TMA into a buffer of the warp's, a thread has a token (its channels lie
-// together, so that one Philox call serves eight of them), y goes back over the residual in shared memory
-// and out by TMA, z beside it.  The TMA clips what hangs over the last token and channel.
+// together, so that one Philox call serves eight of them), and y goes back over the residual in shared memory
+// and from there to memory, eight lanes along a row (a TMA store of 128-byte rows moves 26 GB/s from an SM).
 #include "layer_math.cuh"
 #include "ptx_sm100.cuh"
 
@@ -22,38 +22,49 @@ namespace {
 
 constexpr int kBM = 128, kBK = 64;
 constexpr int kABytes = kBM * kBK * 2;
-constexpr int kEpilogueWarps = 8;
+constexpr int kEpilogueWarps = 16, kPerQuarter = kEpilogueWarps / 4;
 constexpr int kThreads = (2 + kEpilogueWarps) * 32;
 constexpr int kBoxBytes = 32 * 64 * 2;                       // 32 tokens x 64 channels
-constexpr int kBufBytes = kEpilogueWarps * 2 * kBoxBytes;    // two a warp
+constexpr int kBiasBytes = 64 * 4;
+constexpr int kBufBytes = kEpilogueWarps * (kBoxBytes + kBiasBytes);
 constexpr int kMaxStages = 8;
-constexpr int kBarBytes = 256;
+constexpr int kBarBytes = 512;
 constexpr int kSmemMax = 227 * 1024;
 constexpr uint32_t kTmemCols = 512, kSlotCols = 256;
 constexpr uint32_t kSite = 8u << 16;
 
 struct Params {
-  const __nv_bfloat16* bias;
+  const __nv_bfloat16 *bias, *residual_rows;   // (the latter: read without a tensor map)
+  __nv_bfloat16 *y, *z;
   long long rows;
+  int64_t pr, py, pz;
   int32_t Cout, BN, num_kb, tiles_n, tiles, stages, stage_bytes;
-  int32_t residual, keep_z, test_stall;
+  int32_t residual, test_stall;
   int64_t first, step;
   Drop drop;
   uint32_t* status;
 };
 struct Maps {
-  CUtensorMap x, W, residual, y, z;
+  CUtensorMap x, W, residual;
 };
 
-__device__ __forceinline__ void store_2d(const CUtensorMap* m, const void* src, int32_t x, int32_t y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(m)),
-               "r"(ptx::smem_u32(src)), "r"(x), "r"(y)
-               : "memory");
+// Writes a warp's rows of `pieces` 16-byte pieces, from piece `from` on, out of its buffer (rows of 128 bytes, piece c of
+// row i at c ^ (i & 7)): lanes along the rows, as far as the matrix goes.
+template <int PIECES>
+__device__ __forceinline__ void write_rows(const uint8_t* buf, int from, __nv_bfloat16* out, int64_t pitch, int rows, int cols,
+                                           int lane) {
+  constexpr int kRows = 32 / PIECES;   // of an instruction
+  const int piece = lane % PIECES, first = lane / PIECES;
+  __nv_bfloat16* to = out + first * pitch + piece * 8;
+  const bool in = piece * 8 < cols;
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int row = i * kRows + first;
+    const uint4 w = *reinterpret_cast<const uint4*>(buf + row * 128 + (((from + piece) ^ (row & 7)) << 4));
+    if (in && row < rows) *reinterpret_cast<uint4*>(to) = w;
+    to += kRows * pitch;
+  }
 }
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 template <int ACT, bool DROP, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -189,115 +200,116 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     // =========================== epilogue ===========================
-    const int e = warp - 2, sub = e >> 2, quarter = warp & 3;
-    uint8_t* const mine = bufs + e * 2 * kBoxBytes;
+    using V = Vec<__nv_bfloat16>;
+    const int e = warp - 2, quarter = warp & 3;
+    uint8_t* const buf = bufs + e * kBoxBytes;
+    float* const bias = reinterpret_cast<float*>(bufs + kEpilogueWarps * kBoxBytes + e * kBiasBytes);
     const Stream stream = DROP ? open_stream(p.drop) : Stream{};
     if (blockIdx.x == 0 && warp == 2 && lane == 0) note_used(p.drop);
-    uint32_t uses = 0;   // residuals fetched
+    const int chunks = p.BN / 64;
+    const bool keep_z = p.z != nullptr;
+    uint32_t fetched = 0;   // residuals
     bool ok = true;
     int n = 0;
-    const int chunks = p.BN / 64;
     for (int t = unit; t < p.tiles && ok; t += units, ++n) {
-      const int m = t / p.tiles_n;
+      const int m = t / p.tiles_n, c = ((e >> 2) + n) % kPerQuarter;   // (in turn, where there are fewer chunks than warps)
       const long long row0 = static_cast<long long>(m * kCtas + rank) * kBM + quarter * 32;
-      const int col0 = (t - m * p.tiles_n) * p.BN;
-      const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols;
-      bool waited = false;
-      int last = -1;   // this warp's last chunk of the tile
-      for (int c = sub; c < chunks; c += 2) last = c;
-      for (int c = sub; c < chunks; c += 2) {
-        const int col = col0 + c * 64;
-        const bool any = row0 < p.rows && col < p.Cout;
-        uint8_t* const ybuf = mine + ((uses & 1u) && !p.keep_z ? kBoxBytes : 0);
-        if (any) {
-          if (lane == 0) {
-            bulk_wait_read();   // the buffers are free
-            if (p.residual) {
-              ptx::mbar_expect_tx(&arrived[e], kBoxBytes);
-              ptx::tma_load_2d(ybuf, &tm.residual, &arrived[e], col, static_cast<int32_t>(row0));
-            }
-          }
-          __syncwarp();
+      const int col = (t - m * p.tiles_n) * p.BN + c * 64;
+      const int rows = row0 < p.rows ? (p.rows - row0 < 32 ? static_cast<int>(p.rows - row0) : 32) : 0;
+      const int cols = c < chunks && col < p.Cout ? (p.Cout - col < 64 ? p.Cout - col : 64) : 0;
+      const bool any = rows > 0 && cols > 0, by_tma = p.residual && !keep_z;
+      if (any) {
+        if (by_tma && lane == 0) {   // (the buffer is free: the warp has read what it held)
+          ptx::mbar_expect_tx(&arrived[e], kBoxBytes);
+          ptx::tma_load_2d(buf, &tm.residual, &arrived[e], col, static_cast<int32_t>(row0));
         }
-        if (!waited) {
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u));
-          waited = true;
-          ptx::tc_fence_after_sync();
-        }
-        if (p.residual && any) ok &= __all_sync(0xffffffffu, ptx::mbar_wait(&arrived[e], uses & 1u, p.status, kSite | 5u));
-        if (!ok) break;
-        const uint64_t number = static_cast<uint64_t>(p.first + (row0 + lane) * p.step + col);
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          uint32_t a[32];
-          ptx::tmem_ld_32x32(acc + c * 64 + h * 32, a);
-          ptx::tmem_ld_wait();
-          if (h == 1 && c == last) {   // the accumulator has been read
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) {
-              if constexpr (PAIR)
-                ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
-              else
-                ptx::mbar_arrive(&acc_empty[n & 1]);
-            }
-          }
-          if (!any) continue;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {   // eight channels at a time
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(a[g * 8 + j]);
-            const int ch = col + h * 32 + g * 8;
-            if (p.bias != nullptr) {
-              uint4 w = make_uint4(0u, 0u, 0u, 0u);
-              if (ch < p.Cout) w = __ldg(reinterpret_cast<const uint4*>(p.bias + ch));
-              float b[8];
-              Vec<__nv_bfloat16>::unpack(w, b);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] += b[j];
-            }
-            const int at = lane * 128 + (((h * 4 + g) ^ (lane & 7)) << 4);
-            if (p.keep_z) *reinterpret_cast<uint4*>(mine + kBoxBytes + at) = Vec<__nv_bfloat16>::pack(v);
-            if constexpr (ACT != LBP_ACT_NONE) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = act<ACT, true>(v[j]);
-            }
-            if constexpr (DROP) drop(v, number + h * 32 + g * 8, stream, p.drop);
-            if (p.residual) {
-              float r[8];
-              Vec<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(ybuf + at), r);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] += r[j];
-            }
-            *reinterpret_cast<uint4*>(ybuf + at) = Vec<__nv_bfloat16>::pack(v);
-          }
-        }
-        if (any) {
-          ptx::fence_proxy_async_smem();   // the stores read through the async proxy
-          __syncwarp();
-          if (lane == 0) {
-            store_2d(&tm.y, ybuf, col, static_cast<int32_t>(row0));
-            if (p.keep_z) store_2d(&tm.z, mine + kBoxBytes, col, static_cast<int32_t>(row0));
-            bulk_commit();
-          }
-          ++uses;
+        if (p.bias != nullptr) {
+          const uint32_t w = 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
+          *reinterpret_cast<float2*>(bias + 2 * lane) = make_float2(bf16_lo(w), bf16_hi(w));
         }
       }
-      if (last < 0) {   // a tile of one chunk: nothing of it is this warp's
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 6u));
-        if (lane == 0 && ok) {
-          if constexpr (PAIR)
-            ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
-          else
-            ptx::mbar_arrive(&acc_empty[n & 1]);
+      __syncwarp();
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u));
+      ptx::tc_fence_after_sync();
+      if (any && by_tma) {
+        ok &= __all_sync(0xffffffffu, ptx::mbar_wait(&arrived[e], fetched & 1u, p.status, kSite | 5u));
+        ++fetched;
+      }
+      if (!ok) break;
+      const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols + c * 64;
+      const uint64_t number = static_cast<uint64_t>(p.first + (row0 + lane) * p.step + col);
+#pragma unroll 1
+      for (int h = 0; h < 4; ++h) {   // 16 channels
+        uint32_t a[16];
+        if (any) {
+          ptx::tmem_ld_32x16(acc + h * 16, a);
+          ptx::tmem_ld_wait();
         }
+        if (h == 3) {   // the accumulator has been read
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR)
+              ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
+            else
+              ptx::mbar_arrive(&acc_empty[n & 1]);
+          }
+        }
+        if (!any) continue;
+        uint32_t w[8];
+        if constexpr (DROP) {
+          const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
+          philox<2>(stream, group, w);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {   // eight channels at a time
+          float v[8], out[8] = {};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(a[g * 8 + j]);
+          if (p.bias != nullptr) {
+            const float4 b0 = *reinterpret_cast<const float4*>(bias + h * 16 + g * 8);
+            const float4 b1 = *reinterpret_cast<const float4*>(bias + h * 16 + g * 8 + 4);
+            v[0] += b0.x, v[1] += b0.y, v[2] += b0.z, v[3] += b0.w;
+            v[4] += b1.x, v[5] += b1.y, v[6] += b1.z, v[7] += b1.w;
+          }
+          uint8_t* const row = buf + lane * 128;
+          // z and y of 32 channels side by side, or y of 64
+          if (keep_z) *reinterpret_cast<uint4*>(row + ((((h & 1) * 2 + g) ^ (lane & 7)) << 4)) = V::pack(v);
+          uint4* const at = reinterpret_cast<uint4*>(row + ((((keep_z ? 4 + (h & 1) * 2 : h * 2) + g) ^ (lane & 7)) << 4));
+          if (by_tma) {
+            V::unpack(*at, out);
+          } else if (p.residual && lane < rows && h * 16 + g * 8 < cols) {
+            V::unpack(*reinterpret_cast<const uint4*>(p.residual_rows + (row0 + lane) * p.pr + col + h * 16 + g * 8), out);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = act<ACT, true>(v[j]);
+          if constexpr (DROP) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[4 * g + j], p.drop);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) out[j] += v[j];
+          }
+          *at = V::pack(out);
+        }
+        if (keep_z && (h & 1)) {
+          __syncwarp();
+          const int done = (h - 1) * 16;
+          write_rows<4>(buf, 0, p.z + row0 * p.pz + col + done, p.pz, rows, cols - done, lane);
+          write_rows<4>(buf, 4, p.y + row0 * p.py + col + done, p.py, rows, cols - done, lane);
+          __syncwarp();
+        }
+      }
+      if (any && !keep_z) {
+        __syncwarp();
+        write_rows<8>(buf, 0, p.y + row0 * p.py + col, p.py, rows, cols, lane);
+        ptx::fence_proxy_async_smem();   // (the next residual is written through the async proxy)
+        __syncwarp();
       }
       if (*abort_flag != 0) ok = false;
       ok = __all_sync(0xffffffffu, ok);
     }
     if (!ok && lane == 0) *abort_flag = 1;
-    if (lane == 0) bulk_wait_all();
   }
 
   ptx::tc_fence_before_sync();
@@ -370,7 +382,12 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   const int room = kSmemMax - 1024 - kBarBytes - kBufBytes;
   p.stages = room / p.stage_bytes < kMaxStages ? room / p.stage_bytes : kMaxStages;
   p.residual = c.residual != nullptr;
-  p.keep_z = c.z != nullptr;
+  p.residual_rows = static_cast<const __nv_bfloat16*>(c.residual);
+  p.y = static_cast<__nv_bfloat16*>(c.y);
+  p.z = static_cast<__nv_bfloat16*>(c.z);
+  p.pr = c.pr;
+  p.py = c.py;
+  p.pz = c.pz;
   p.test_stall = g_test_stall ? 1 : 0;
   p.first = c.first;
   p.step = c.step;
@@ -379,12 +396,9 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   Maps tm;
   if (int e = encode_matrix_tensor_map(&tm.x, c.x, c.rows, c.Cin, kBM, c.px)) return e;
   if (int e = encode_matrix_tensor_map(&tm.W, c.W, c.Cout, c.Cin, part)) return e;
-  if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py)) return e;
-  tm.residual = tm.z = tm.y;
-  if (c.residual != nullptr)
+  tm.residual = tm.x;
+  if (c.residual != nullptr && c.z == nullptr)
     if (int e = encode_matrix_tensor_map(&tm.residual, c.residual, c.rows, c.Cout, 32, c.pr)) return e;
-  if (c.z != nullptr)
-    if (int e = encode_matrix_tensor_map(&tm.z, c.z, c.rows, c.Cout, 32, c.pz)) return e;
 
   const int units = plan.pair ? sms / 2 : sms;
   cudaLaunchConfig_t cfg = {};

@@ -47,40 +47,60 @@ __device__ __forceinline__ void note_used(const Drop& d) {
   d.used[1] = offset;
 }
 
-// Philox4x32-10 (Salmon et al. 2011): the numbers of elements 8 group .. 8 group + 7, two a word.
-__device__ __forceinline__ uint4 philox(const Stream& s, uint64_t group) {
-  uint32_t c0 = static_cast<uint32_t>(group), c1 = static_cast<uint32_t>(group >> 32), c2 = s.c2, c3 = s.c3;
+// Philox4x32-10 (Salmon et al. 2011): the numbers of elements 8 group .. 8 group + 7, two a word, for G
+// groups at once, which hides the rounds' latency and shares the key's additions.
+template <int G>
+__device__ __forceinline__ void philox(const Stream& s, const uint64_t (&group)[G], uint32_t (&w)[4 * G]) {
   uint32_t k0 = s.k0, k1 = s.k1;
 #pragma unroll
+  for (int g = 0; g < G; ++g) {
+    w[4 * g] = static_cast<uint32_t>(group[g]);
+    w[4 * g + 1] = static_cast<uint32_t>(group[g] >> 32);
+    w[4 * g + 2] = s.c2;
+    w[4 * g + 3] = s.c3;
+  }
+#pragma unroll
   for (int r = 0; r < 10; ++r) {
-    const uint64_t a = static_cast<uint64_t>(c0) * 0xD2511F53u, b = static_cast<uint64_t>(c2) * 0xCD9E8D57u;
-    c0 = static_cast<uint32_t>(b >> 32) ^ c1 ^ k0;
-    c1 = static_cast<uint32_t>(b);
-    c2 = static_cast<uint32_t>(a >> 32) ^ c3 ^ k1;
-    c3 = static_cast<uint32_t>(a);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      uint32_t* const c = w + 4 * g;
+      const uint64_t a = static_cast<uint64_t>(c[0]) * 0xD2511F53u, b = static_cast<uint64_t>(c[2]) * 0xCD9E8D57u;
+      c[0] = static_cast<uint32_t>(b >> 32) ^ c[1] ^ k0;
+      c[1] = static_cast<uint32_t>(b);
+      c[2] = static_cast<uint32_t>(a >> 32) ^ c[3] ^ k1;
+      c[3] = static_cast<uint32_t>(a);
+    }
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  return make_uint4(c0, c1, c2, c3);
 }
-// Drops among the elements whose numbers are the low and the high half of w.
-__device__ __forceinline__ void drop2(float& lo, float& hi, uint32_t w, const Drop& d) {
-  lo = (w << 16) > d.above ? lo * d.scale : 0.f;
-  hi = w > d.above ? hi * d.scale : 0.f;
+// acc += scale * v where the number in the high half of w is above the bound: a predicated multiply-add,
+// which leaves what is dropped out of the sum, whatever it is.
+__device__ __forceinline__ void add_kept(float& acc, float v, uint32_t w, const Drop& d) {
+  asm("{\n\t.reg .pred p;\n\t"
+      "setp.gt.u32 p, %2, %3;\n\t"
+      "@p fma.rn.f32 %0, %1, %4, %0;\n\t}"
+      : "+f"(acc)
+      : "f"(v), "r"(w), "r"(d.above), "f"(d.scale));
 }
-// Elements n .. n + 7 (n a multiple of 8), or n .. n + 3 (of 4).
-__device__ __forceinline__ void drop(float (&v)[8], uint64_t n, const Stream& s, const Drop& d) {
-  const uint4 w = philox(s, n >> 3);
-  drop2(v[0], v[1], w.x, d);
-  drop2(v[2], v[3], w.y, d);
-  drop2(v[4], v[5], w.z, d);
-  drop2(v[6], v[7], w.w, d);
+__device__ __forceinline__ void add_kept2(float& lo, float& hi, float v0, float v1, uint32_t w, const Drop& d) {
+  add_kept(lo, v0, w << 16, d);
+  add_kept(hi, v1, w, d);
 }
-__device__ __forceinline__ void drop(float (&v)[4], uint64_t n, const Stream& s, const Drop& d) {
-  const uint4 w = philox(s, n >> 3);
-  const bool upper = (n & 4u) != 0;
-  drop2(v[0], v[1], upper ? w.z : w.x, d);
-  drop2(v[2], v[3], upper ? w.w : w.y, d);
+
+// out += drop(v) of four elements from number n (a multiple of 4) on.
+__device__ __forceinline__ void add_dropped(float (&out)[4], const float (&v)[4], uint64_t n, const Stream& s, const Drop& d) {
+  if (d.on) {
+    const uint64_t group[1] = {n >> 3};
+    uint32_t w[4];
+    philox<1>(s, group, w);
+    const bool upper = (n & 4u) != 0;
+    add_kept2(out[0], out[1], v[0], v[1], upper ? w[2] : w[0], d);
+    add_kept2(out[2], out[3], v[2], v[3], upper ? w[3] : w[1], d);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] += v[j];
+  }
 }
 
 // ---- activations ------------------------------------------------------------------------
@@ -110,19 +130,30 @@ constexpr float kLog2e = 1.4426950408889634f;
 // 2 sqrt(2/pi) and 0.044715 times that: gelu_tanh(z) = z / (1 + exp(-(A z + B z^3)))
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.071354816272600247f;
 
-// Phi(-a) = exp(-a^2/2) Q(t) with t = 1 / (1 + 0.38 a): a polynomial of degree 5 fitted to
-// exp(a^2/2) erfc(a / sqrt 2) / 2 in the relative error, 3.7e-5 at most over a = 0..40.  Also
-// hands out e = exp(-a^2/2).
-__device__ __forceinline__ float upper_tail(float a, float* e) {
+// The normal distribution's tail Phi(-a), a >= 0, as exp(-a^2/2) times a polynomial in t = 1 / (1 + c a), fitted
+// (weighted least squares towards the smallest largest error):
+//   exp(a^2/2) a Phi(-a) = S(t), c = 0.4, off by at most 8.6e-5 (S + 0.002).  With it gelu(z) =
+//       max(z, 0) - |z| Phi(-|z|) needs no case for infinities: t, exp(-a^2/2) and S stay finite.
+//   exp(a^2/2) Phi(-a) = Q(t), c = 0.38, off by at most 3.7e-5 Q.
+__device__ __forceinline__ float tail_times_a(float a, float z) {
+  const float t = rcp(fmaf(0.4f, a, 1.f));
+  const float e = ex2(z * (z * (-0.5f * kLog2e)));
+  float q = 0.2135479748249054f;
+  q = fmaf(q, t, -0.5766780972480774f);
+  q = fmaf(q, t, 0.06343623995780945f);
+  q = fmaf(q, t, -0.10194139182567596f);
+  q = fmaf(q, t, 0.0027213171124458313f);
+  q = fmaf(q, t, 0.3989139497280121f);
+  return q * e;
+}
+__device__ __forceinline__ float tail_poly(float a) {
   const float t = rcp(fmaf(0.38f, a, 1.f));
-  *e = ex2(a * (a * (-0.5f * kLog2e)));
   float q = -0.0906074270606041f;
   q = fmaf(q, t, 0.1908050775527954f);
   q = fmaf(q, t, 0.08993600308895111f);
   q = fmaf(q, t, 0.15882457792758942f);
   q = fmaf(q, t, 0.15100638568401337f);
-  q = fmaf(q, t, 1.705829163256567e-05f);
-  return q * *e;
+  return fmaf(q, t, 1.705829163256567e-05f);
 }
 
 // FAST: for results that are rounded to bf16.
@@ -134,10 +165,7 @@ __device__ __forceinline__ float act(float z) {
     return at_least(z, 0.f);
   } else if constexpr (ACT == LBP_ACT_GELU) {
     if constexpr (FAST) {
-      const float a = at_most(fabsf(z), 100.f);
-      float e;
-      const float tail = upper_tail(a, &e);
-      return fmaf(-a, tail, fmaxf(z, 0.f));   // (a NaN comes through a)
+      return fmaxf(z, 0.f) - tail_times_a(fabsf(z), z);   // (a NaN comes through the tail)
     } else {
       const float c = at_least(z, -100.f);
       return 0.5f * c * erfcf(c * -0.70710678118654752f);
@@ -167,10 +195,11 @@ __device__ __forceinline__ float act_slope(float z) {
     return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;   // (NaN stays)
   } else if constexpr (ACT == LBP_ACT_GELU) {
     if constexpr (FAST) {
-      const float c = at_most(at_least(z, -100.f), 100.f);
-      float e;
-      const float tail = upper_tail(fabsf(c), &e);
-      return fmaf(c * kInvSqrt2Pi, e, c > 0.f ? 1.f - tail : tail);
+      // Phi(z) + z phi(z) = 1/2 + sign(z) (1/2 - g), g = exp(-a^2/2) (Q - a / sqrt(2 pi)) <= 1/2, a = |z|
+      const float a = at_most(fabsf(z), 100.f);
+      const float e = ex2(a * (a * (-0.5f * kLog2e)));
+      const float d = fmaf(-e, fmaf(-kInvSqrt2Pi, a, tail_poly(a)), 0.5f);
+      return 0.5f + copysignf(d, z);
     } else {
       const float c = at_most(at_least(z, -100.f), 100.f);
       return fmaf(c * kInvSqrt2Pi, expf(-0.5f * c * c), 0.5f * erfcf(c * -0.70710678118654752f));
@@ -249,7 +278,8 @@ struct LinearCall {
 int launch_linear(const LinearCall& c, cudaStream_t stream);
 int launch_linear_umma(const LinearCall& c, cudaStream_t stream);   // bf16
 
-// out = residual + drop(a) act'(z) on the tokens of a grid (rows: H = W = 1)
+// out = residual + drop(a) act'(z) on the tokens of a grid (rows: H = W = 1).  At most one of z and
+// residual.
 struct PointCall {
   const void *a, *z, *residual;
   void* out;

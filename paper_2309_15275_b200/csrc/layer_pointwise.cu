@@ -1,54 +1,155 @@
 // out = residual + drop(a) act'(z): dropout on its own, and the gradient of a layer's epilogue.
+//
+// One pass; a thread has kVectors vectors of 16 bytes of each tensor, 256 threads apart, and asks for all of
+// them before it computes.  Bound by memory where the arithmetic is light; with dropout by issue: a
+// Philox call is 20 multiplications and 20 xor's for eight elements (fp32 data: for four).
 #include "layer_math.cuh"
 
 namespace lbp {
 namespace layer {
 
-template <class T, int ACT>
-__global__ void __launch_bounds__(256) pointwise_kernel(const __grid_constant__ PointCall p) {
+// vectors of a thread: with few, more blocks have work; with many, more loads are under way
+constexpr int kVectors = 4;
+
+// n / d for n < 2^31 without a division: magic numbers from the host (Granlund and Montgomery 1994).
+struct Divisor {
+  uint32_t d, mul, shift;
+};
+static Divisor divisor(uint32_t d) {
+  uint32_t shift = 0;
+  while ((1ull << shift) < d) ++shift;
+  return Divisor{d, static_cast<uint32_t>(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Divisor& v) {
+  return static_cast<uint32_t>((static_cast<uint64_t>(__umulhi(n, v.mul)) + n) >> v.shift);
+}
+
+struct Grid {
+  long long vectors;
+  Divisor per_row, HW, W;
+};
+
+// FLAT: every tensor, and the numbering, is one run of memory.
+template <class T, int ACT, bool DROP, bool FLAT, int U>
+__global__ void __launch_bounds__(256) pointwise_kernel(const __grid_constant__ PointCall p, const __grid_constant__ Grid grid) {
   using V = Vec<T>;
-  const Stream s = open_stream(p.drop);
+  const long long i0 = blockIdx.x * (256ll * U) + threadIdx.x;
+  // (the kernel ahead may still write what is read here)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Stream s = DROP ? open_stream(p.drop) : Stream{};
   if (blockIdx.x == 0 && threadIdx.x == 0) note_used(p.drop);
-  const int per_row = p.C / V::N;
-  const long long n = p.rows * per_row;
-  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-    const long long row = i / per_row;
-    const int c = static_cast<int>(i - row * per_row) * V::N;
-    const long long b = row / p.HW;
-    const int t = static_cast<int>(row - b * p.HW), h = t / p.W, w = t - h * p.W;
-    auto at = [&](const lbp_view& v) { return b * v.image + h * v.row + w * v.token + c; };
-    float v[V::N];
-    V::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.a) + at(p.va)), v);
+  uint4 a[U], z[U];
+  uint64_t number[U];
+  int64_t out[U];
+  const T* const second = static_cast<const T*>(ACT != LBP_ACT_NONE ? p.z : p.residual);
+  const lbp_view& v2 = ACT != LBP_ACT_NONE ? p.vz : p.vr;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long long i = i0 + u * 256;
+    if (i >= grid.vectors) break;
+    int64_t at, at2;
+    if constexpr (FLAT) {
+      at = at2 = out[u] = i * V::N;
+      number[u] = p.first + at;
+    } else {
+      long long row, b;
+      if (grid.vectors < (1ll << 31)) {
+        row = quotient(static_cast<uint32_t>(i), grid.per_row);
+        b = quotient(static_cast<uint32_t>(row), grid.HW);
+      } else {
+        row = i / grid.per_row.d;
+        b = row / p.HW;
+      }
+      const int c = static_cast<int>(i - row * grid.per_row.d) * V::N;
+      const uint32_t t = static_cast<uint32_t>(row - b * p.HW), h = quotient(t, grid.W), w = t - h * p.W;
+      auto where = [&](const lbp_view& v) { return b * v.image + h * v.row + w * v.token + c; };
+      at = where(p.va);
+      at2 = second != nullptr ? where(v2) : 0;
+      out[u] = where(p.vo);
+      number[u] = p.first + where(p.number);
+    }
+    a[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(p.a) + at));
+    if (second != nullptr) z[u] = __ldcs(reinterpret_cast<const uint4*>(second + at2));
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (i0 + u * 256 >= grid.vectors) break;
+    float v[V::N], r[V::N] = {};
+    V::unpack(a[u], v);
     if constexpr (ACT != LBP_ACT_NONE) {
-      float z[V::N];
-      V::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.z) + at(p.vz)), z);
+      float x[V::N];
+      V::unpack(z[u], x);
 #pragma unroll
-      for (int j = 0; j < V::N; ++j) v[j] *= act_slope<ACT, V::kFast>(z[j]);
+      for (int j = 0; j < V::N; ++j) v[j] *= act_slope<ACT, V::kFast>(x[j]);
+    } else if (second != nullptr) {
+      V::unpack(z[u], r);
     }
-    if (p.drop.on) drop(v, p.first + at(p.number), s, p.drop);
-    if (p.residual != nullptr) {
-      float r[V::N];
-      V::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.residual) + at(p.vr)), r);
+    if constexpr (DROP) {
+      const uint64_t group[1] = {number[u] >> 3};
+      uint32_t w[4];
+      philox<1>(s, group, w);
+      if constexpr (V::N == 8) {
 #pragma unroll
-      for (int j = 0; j < V::N; ++j) v[j] += r[j];
+        for (int j = 0; j < 4; ++j) add_kept2(r[2 * j], r[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
+      } else {
+        const bool upper = (number[u] & 4u) != 0;
+        add_kept2(r[0], r[1], v[0], v[1], upper ? w[2] : w[0], p.drop);
+        add_kept2(r[2], r[3], v[2], v[3], upper ? w[3] : w[1], p.drop);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V::N; ++j) r[j] += v[j];
     }
-    *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + at(p.vo)) = V::pack(v);
+    *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + out[u]) = V::pack(r);
   }
 }
 
-int launch_pointwise(const PointCall& c, cudaStream_t stream) {
-  const int per_row = c.C / (c.dtype == LBP_BF16 ? 8 : 4);
-  const long long n = c.rows * per_row, blocks = (n + 255) / 256;
-  const unsigned grid = static_cast<unsigned>(blocks < 148 * 32 ? blocks : 148 * 32);
-  return with_act(c.act, [&](auto a) -> int {
-    constexpr int ACT = decltype(a)::value;
+int launch_pointwise(const PointCall& call, cudaStream_t stream) {
+  PointCall c = call;
+  const int N = c.dtype == LBP_BF16 ? 8 : 4;
+  const int H = c.HW / c.W;
+  // rows that lie one behind the other are one row
+  auto one_run = [&](const lbp_view& v) {
+    return (c.W == 1 || v.token == c.C) && (H == 1 || v.row == static_cast<int64_t>(c.W) * c.C) &&
+           (c.rows == c.HW || v.image == static_cast<int64_t>(c.HW) * c.C);
+  };
+  const bool flat = one_run(c.va) && one_run(c.vo) && one_run(c.number) && (c.z == nullptr || one_run(c.vz)) &&
+                    (c.residual == nullptr || one_run(c.vr));
+  Grid g{};
+  g.vectors = c.rows * (c.C / N);
+  g.per_row = divisor(static_cast<uint32_t>(c.C / N));
+  g.HW = divisor(static_cast<uint32_t>(c.HW));
+  g.W = divisor(static_cast<uint32_t>(c.W));
+  const int per = g.vectors >= 148ll * 2048 * kVectors ? kVectors : 1;   // (all SMs full of threads)
+  const long long blocks = (g.vectors + 256ll * per - 1) / (256ll * per);
+  if (blocks >= (1ll << 31)) return LBP_ERR_SHAPE;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return with_act(c.act, [&](auto act) -> int {
+    constexpr int ACT = decltype(act)::value;
+    auto go = [&](auto t, auto drop, auto f) -> int {
+      using T = decltype(t);
+      constexpr bool DROP = decltype(drop)::value, FLAT = decltype(f)::value;
+      if (per == 1)
+        LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, pointwise_kernel<T, ACT, DROP, FLAT, 1>, c, g));
+      else
+        LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, pointwise_kernel<T, ACT, DROP, FLAT, kVectors>, c, g));
+      count_launch();
+      return LBP_OK;
+    };
+    auto by_drop = [&](auto t, auto f) -> int {
+      return c.drop.on ? go(t, std::true_type{}, f) : go(t, std::false_type{}, f);
+    };
     if (c.dtype == LBP_BF16)
-      pointwise_kernel<__nv_bfloat16, ACT><<<grid, 256, 0, stream>>>(c);
-    else
-      pointwise_kernel<float, ACT><<<grid, 256, 0, stream>>>(c);
-    count_launch();
-    LBP_CUDA_TRY(cudaGetLastError());
-    return LBP_OK;
+      return flat ? by_drop(__nv_bfloat16{}, std::true_type{}) : by_drop(__nv_bfloat16{}, std::false_type{});
+    return flat ? by_drop(float{}, std::true_type{}) : by_drop(float{}, std::false_type{});
   });
 }
 
