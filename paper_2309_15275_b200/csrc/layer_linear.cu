@@ -8,7 +8,6 @@ constexpr int kTile = 64, kDepth = 16;
 
 template <class T, int ACT>
 __global__ void __launch_bounds__(256) linear_tile_kernel(const __grid_constant__ LinearCall p) {
-  using V = Vec<T>;
   __shared__ float xs[kDepth][kTile + 4], ws[kDepth][kTile + 4];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const unsigned across = (p.Cout + kTile - 1) / kTile;
@@ -50,7 +49,7 @@ __global__ void __launch_bounds__(256) linear_tile_kernel(const __grid_constant_
       v[j] = acc[i][j];
       if (p.bias != nullptr) v[j] += static_cast<float>(static_cast<const T*>(p.bias)[c + j]);
       if (p.z != nullptr) static_cast<T*>(p.z)[row * p.pz + c + j] = static_cast<T>(v[j]);
-      v[j] = act<ACT, V::kFast>(v[j]);
+      v[j] = act<ACT>(v[j]);
     }
     float out[4] = {};
     if (p.residual != nullptr) {

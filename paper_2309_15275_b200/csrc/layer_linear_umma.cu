@@ -8,10 +8,11 @@
 // next to one another, so that x comes from HBM once and W stays in L2.
 //
 // Warps: 0 TMA loads, 1 tcgen05, 2-17 the epilogue, four to each quarter of the accumulator's lanes, which
-// take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels: the
-// residual comes by TMA into a buffer of the warp's, a thread has a token (its channels lie
-// together, so that one Philox call serves eight of them), and y goes back over the residual in shared memory
-// and from there to memory, eight lanes along a row (a TMA store of 128-byte rows moves 26 GB/s from an SM).
+// take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels.  A
+// thread has a token, so that its channels lie together: one Philox call serves eight of them, and 16 are 32 bytes, a
+// whole sector, which it writes (and reads of the residual) in one instruction.  A warp's 32 rows of 32 bytes move 5.6
+// TB/s from all SMs, rows of 128 bytes by way of shared memory 6.1 (16-byte pieces 1.65, TMA stores of 128-byte
+// rows 3.5); what the way through shared memory costs in instructions is more.
 #include "layer_math.cuh"
 #include "ptx_sm100.cuh"
 
@@ -24,61 +25,65 @@ constexpr int kBM = 128, kBK = 64;
 constexpr int kABytes = kBM * kBK * 2;
 constexpr int kEpilogueWarps = 16, kPerQuarter = kEpilogueWarps / 4;
 constexpr int kThreads = (2 + kEpilogueWarps) * 32;
-constexpr int kBoxBytes = 32 * 64 * 2;                       // 32 tokens x 64 channels
-constexpr int kBiasBytes = 64 * 4;
-constexpr int kBufBytes = kEpilogueWarps * (kBoxBytes + kBiasBytes);
+constexpr int kBiasBytes = kEpilogueWarps * 64 * 4;   // a chunk's, for each warp
 constexpr int kMaxStages = 8;
-constexpr int kBarBytes = 512;
+constexpr int kBarBytes = 256;
 constexpr int kSmemMax = 227 * 1024;
 constexpr uint32_t kTmemCols = 512, kSlotCols = 256;
 constexpr uint32_t kSite = 8u << 16;
 
 struct Params {
-  const __nv_bfloat16 *bias, *residual_rows;   // (the latter: read without a tensor map)
+  const __nv_bfloat16 *bias, *residual;
   __nv_bfloat16 *y, *z;
   long long rows;
   int64_t pr, py, pz;
   int32_t Cout, BN, num_kb, tiles_n, tiles, stages, stage_bytes;
-  int32_t residual, test_stall;
+  int32_t wide, test_stall;   // rows of y, z and the residual start on 32-byte boundaries
   int64_t first, step;
   Drop drop;
   uint32_t* status;
 };
 struct Maps {
-  CUtensorMap x, W, residual;
+  CUtensorMap x, W;
 };
 
-// Writes a warp's rows of `pieces` 16-byte pieces, from piece `from` on, out of its buffer (rows of 128 bytes, piece c of
-// row i at c ^ (i & 7)): lanes along the rows, as far as the matrix goes.
-template <int PIECES>
-__device__ __forceinline__ void write_rows(const uint8_t* buf, int from, __nv_bfloat16* out, int64_t pitch, int rows, int cols,
-                                           int lane) {
-  constexpr int kRows = 32 / PIECES;   // of an instruction
-  const int piece = lane % PIECES, first = lane / PIECES;
-  __nv_bfloat16* to = out + first * pitch + piece * 8;
-  const bool in = piece * 8 < cols;
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int row = i * kRows + first;
-    const uint4 w = *reinterpret_cast<const uint4*>(buf + row * 128 + (((from + piece) ^ (row & 7)) << 4));
-    if (in && row < rows) *reinterpret_cast<uint4*>(to) = w;
-    to += kRows * pitch;
+// 16 channels of a row, as far as they go (`n` of them), to and from registers.
+__device__ __forceinline__ void write16(__nv_bfloat16* to, const uint32_t (&w)[8], int n, bool wide) {
+  if (wide && n >= 16) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    if (n > 0) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (n > 8) *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+__device__ __forceinline__ void read16(const __nv_bfloat16* from, uint32_t (&w)[8], int n, bool wide) {
+  if (wide && n >= 16) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(from)
+                 : "memory");
+  } else {
+    uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+    if (n > 0) a = *reinterpret_cast<const uint4*>(from);
+    if (n > 8) b = *reinterpret_cast<const uint4*>(from + 8);
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
   }
 }
 
-template <int ACT, bool DROP, bool PAIR>
+template <int ACT, bool DROP, bool RES, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_umma_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   constexpr int kCtas = PAIR ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint8_t* const bufs = smem + p.stages * p.stage_bytes;
-  uint64_t* const full = reinterpret_cast<uint64_t*>(bufs + kBufBytes);   // [kMaxStages]
+  float* const biases = reinterpret_cast<float*>(smem + p.stages * p.stage_bytes);
+  uint64_t* const full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(biases) + kBiasBytes);   // [kMaxStages]
   uint64_t* const empty = full + kMaxStages;
   uint64_t* const acc_full = empty + kMaxStages;    // [2]
   uint64_t* const acc_empty = acc_full + 2;         // [2], the leader's are used
-  uint64_t* const arrived = acc_empty + 2;          // [kEpilogueWarps]: a warp's residual
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(arrived + kEpilogueWarps);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -94,7 +99,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&acc_full[s], 1);
       ptx::mbar_init(&acc_empty[s], kCtas * kEpilogueWarps);
     }
-    for (int s = 0; s < kEpilogueWarps; ++s) ptx::mbar_init(&arrived[s], 1);
     ptx::mbar_fence_init();
     *abort_flag = 0;
     ptx::prefetch_tensormap(&tm.x);
@@ -200,114 +204,106 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     // =========================== epilogue ===========================
-    using V = Vec<__nv_bfloat16>;
     const int e = warp - 2, quarter = warp & 3;
-    uint8_t* const buf = bufs + e * kBoxBytes;
-    float* const bias = reinterpret_cast<float*>(bufs + kEpilogueWarps * kBoxBytes + e * kBiasBytes);
+    float* const bias = biases + e * 64;
     const Stream stream = DROP ? open_stream(p.drop) : Stream{};
     if (blockIdx.x == 0 && warp == 2 && lane == 0) note_used(p.drop);
     const int chunks = p.BN / 64;
-    const bool keep_z = p.z != nullptr;
-    uint32_t fetched = 0;   // residuals
     bool ok = true;
     int n = 0;
-    for (int t = unit; t < p.tiles && ok; t += units, ++n) {
+    for (int t = unit; t < p.tiles; t += units, ++n) {
       const int m = t / p.tiles_n, c = ((e >> 2) + n) % kPerQuarter;   // (in turn, where there are fewer chunks than warps)
-      const long long row0 = static_cast<long long>(m * kCtas + rank) * kBM + quarter * 32;
+      const long long row = static_cast<long long>(m * kCtas + rank) * kBM + quarter * 32 + lane;
       const int col = (t - m * p.tiles_n) * p.BN + c * 64;
-      const int rows = row0 < p.rows ? (p.rows - row0 < 32 ? static_cast<int>(p.rows - row0) : 32) : 0;
-      const int cols = c < chunks && col < p.Cout ? (p.Cout - col < 64 ? p.Cout - col : 64) : 0;
-      const bool any = rows > 0 && cols > 0, by_tma = p.residual && !keep_z;
-      if (any) {
-        if (by_tma && lane == 0) {   // (the buffer is free: the warp has read what it held)
-          ptx::mbar_expect_tx(&arrived[e], kBoxBytes);
-          ptx::tma_load_2d(buf, &tm.residual, &arrived[e], col, static_cast<int32_t>(row0));
-        }
-        if (p.bias != nullptr) {
-          const uint32_t w = 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
-          *reinterpret_cast<float2*>(bias + 2 * lane) = make_float2(bf16_lo(w), bf16_hi(w));
-        }
+      const int cols = c < chunks ? p.Cout - col : 0;          // of this chunk on
+      const int mine = row < p.rows ? cols : 0;                // ... in this thread's row
+      if (p.bias != nullptr && cols > 0) {
+        const uint32_t w = 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
+        __syncwarp();   // (everyone has read the last chunk's)
+        *reinterpret_cast<float2*>(bias + 2 * lane) = make_float2(bf16_lo(w), bf16_hi(w));
       }
+      const __nv_bfloat16* const res = p.residual + row * p.pr + col;
+      uint32_t r[8];
+      if constexpr (RES) read16(res, r, mine, p.wide);
       __syncwarp();
-      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u));
-      ptx::tc_fence_after_sync();
-      if (any && by_tma) {
-        ok &= __all_sync(0xffffffffu, ptx::mbar_wait(&arrived[e], fetched & 1u, p.status, kSite | 5u));
-        ++fetched;
-      }
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u) &&
+                                       *abort_flag == 0);
       if (!ok) break;
+      ptx::tc_fence_after_sync();
       const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols + c * 64;
-      const uint64_t number = static_cast<uint64_t>(p.first + (row0 + lane) * p.step + col);
-#pragma unroll 1
-      for (int h = 0; h < 4; ++h) {   // 16 channels
-        uint32_t a[16];
-        if (any) {
-          ptx::tmem_ld_32x16(acc + h * 16, a);
-          ptx::tmem_ld_wait();
-        }
-        if (h == 3) {   // the accumulator has been read
-          ptx::tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) {
-            if constexpr (PAIR)
-              ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
-            else
-              ptx::mbar_arrive(&acc_empty[n & 1]);
+      const uint64_t number = static_cast<uint64_t>(p.first + row * p.step + col);
+      __nv_bfloat16 *const y = p.y + row * p.py + col, *const z = p.z + row * p.pz + col;
+
+      // 16 channels at h * 16, from the accumulator in a
+      auto step = [&](int h, const uint32_t (&a)[16]) {
+        float v[16], out[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(a[j]);
+        if (p.bias != nullptr) {
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias + h * 16 + j);
+            parts(add2(two(v[j], v[j + 1]), two(b.x, b.y)), v[j], v[j + 1]);
+            parts(add2(two(v[j + 2], v[j + 3]), two(b.z, b.w)), v[j + 2], v[j + 3]);
           }
         }
-        if (!any) continue;
+        const int left = mine - h * 16;
         uint32_t w[8];
+        if (p.z != nullptr) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+          write16(z + h * 16, w, left, p.wide);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) act_fast<ACT>(v[j], v[j + 1]);
+        if constexpr (RES) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(r[j]), out[2 * j + 1] = bf16_hi(r[j]);
+          if (h < 3) read16(res + (h + 1) * 16, r, left - 16, p.wide);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) out[j] = 0.f;
+        }
         if constexpr (DROP) {
           const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
           philox<2>(stream, group, w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
+        } else if constexpr (RES) {
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) parts(add2(two(out[j], out[j + 1]), two(v[j], v[j + 1])), out[j], out[j + 1]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) out[j] = v[j];
         }
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {   // eight channels at a time
-          float v[8], out[8] = {};
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(a[g * 8 + j]);
-          if (p.bias != nullptr) {
-            const float4 b0 = *reinterpret_cast<const float4*>(bias + h * 16 + g * 8);
-            const float4 b1 = *reinterpret_cast<const float4*>(bias + h * 16 + g * 8 + 4);
-            v[0] += b0.x, v[1] += b0.y, v[2] += b0.z, v[3] += b0.w;
-            v[4] += b1.x, v[5] += b1.y, v[6] += b1.z, v[7] += b1.w;
-          }
-          uint8_t* const row = buf + lane * 128;
-          // z and y of 32 channels side by side, or y of 64
-          if (keep_z) *reinterpret_cast<uint4*>(row + ((((h & 1) * 2 + g) ^ (lane & 7)) << 4)) = V::pack(v);
-          uint4* const at = reinterpret_cast<uint4*>(row + ((((keep_z ? 4 + (h & 1) * 2 : h * 2) + g) ^ (lane & 7)) << 4));
-          if (by_tma) {
-            V::unpack(*at, out);
-          } else if (p.residual && lane < rows && h * 16 + g * 8 < cols) {
-            V::unpack(*reinterpret_cast<const uint4*>(p.residual_rows + (row0 + lane) * p.pr + col + h * 16 + g * 8), out);
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = act<ACT, true>(v[j]);
-          if constexpr (DROP) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[4 * g + j], p.drop);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) out[j] += v[j];
-          }
-          *at = V::pack(out);
-        }
-        if (keep_z && (h & 1)) {
-          __syncwarp();
-          const int done = (h - 1) * 16;
-          write_rows<4>(buf, 0, p.z + row0 * p.pz + col + done, p.pz, rows, cols - done, lane);
-          write_rows<4>(buf, 4, p.y + row0 * p.py + col + done, p.py, rows, cols - done, lane);
-          __syncwarp();
-        }
+        for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(out[2 * j], out[2 * j + 1]);
+        write16(y + h * 16, w, left, p.wide);
+      };
+      // a step's accumulator is read while the one before is worked on
+      uint32_t a0[16], a1[16];
+      if (cols > 0) {
+        ptx::tmem_ld_32x16(acc, a0);
+        ptx::tmem_ld_wait();
       }
-      if (any && !keep_z) {
-        __syncwarp();
-        write_rows<8>(buf, 0, p.y + row0 * p.py + col, p.py, rows, cols, lane);
-        ptx::fence_proxy_async_smem();   // (the next residual is written through the async proxy)
-        __syncwarp();
+#pragma unroll 1
+      for (int h = 0; h < 4 && cols > 0; h += 2) {
+        ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
+        step(h, a0);
+        ptx::tmem_ld_wait();
+        if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
+        step(h + 1, a1);
+        ptx::tmem_ld_wait();
       }
-      if (*abort_flag != 0) ok = false;
-      ok = __all_sync(0xffffffffu, ok);
+      // the accumulator has been read
+      ptx::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (PAIR)
+          ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
+        else
+          ptx::mbar_arrive(&acc_empty[n & 1]);
+      }
     }
     if (!ok && lane == 0) *abort_flag = 1;
   }
@@ -379,27 +375,24 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   if (tiles >= (1ll << 31)) return LBP_ERR_SHAPE;
   p.tiles = static_cast<int32_t>(tiles);
   p.stage_bytes = kABytes + part * kBK * 2;
-  const int room = kSmemMax - 1024 - kBarBytes - kBufBytes;
+  const int room = kSmemMax - 1024 - kBarBytes - kBiasBytes;
   p.stages = room / p.stage_bytes < kMaxStages ? room / p.stage_bytes : kMaxStages;
-  p.residual = c.residual != nullptr;
-  p.residual_rows = static_cast<const __nv_bfloat16*>(c.residual);
-  p.y = static_cast<__nv_bfloat16*>(c.y);
-  p.z = static_cast<__nv_bfloat16*>(c.z);
-  p.pr = c.pr;
-  p.py = c.py;
-  p.pz = c.pz;
   p.test_stall = g_test_stall ? 1 : 0;
   p.first = c.first;
   p.step = c.step;
   p.drop = c.drop;
   p.status = c.status;
+  p.residual = static_cast<const __nv_bfloat16*>(c.residual);
+  p.y = static_cast<__nv_bfloat16*>(c.y);
+  p.z = static_cast<__nv_bfloat16*>(c.z);
+  p.pr = c.pr;
+  p.py = c.py;
+  p.pz = c.pz;
+  auto wide = [](const void* q, int64_t pitch) { return ((reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(2 * pitch)) & 31u) == 0; };
+  p.wide = wide(c.y, c.py) && (c.z == nullptr || wide(c.z, c.pz)) && (c.residual == nullptr || wide(c.residual, c.pr));
   Maps tm;
   if (int e = encode_matrix_tensor_map(&tm.x, c.x, c.rows, c.Cin, kBM, c.px)) return e;
   if (int e = encode_matrix_tensor_map(&tm.W, c.W, c.Cout, c.Cin, part)) return e;
-  tm.residual = tm.x;
-  if (c.residual != nullptr && c.z == nullptr)
-    if (int e = encode_matrix_tensor_map(&tm.residual, c.residual, c.rows, c.Cout, 32, c.pr)) return e;
-
   const int units = plan.pair ? sms / 2 : sms;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -411,7 +404,7 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(static_cast<unsigned>(ctas * (tiles < units ? tiles : units)));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = 1024 + p.stages * p.stage_bytes + kBufBytes + kBarBytes;
+  cfg.dynamicSmemBytes = 1024 + p.stages * p.stage_bytes + kBiasBytes + kBarBytes;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = plan.pair ? 2 : 1;
@@ -423,12 +416,16 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
       count_launch();
       return LBP_OK;
     };
-    static PerDevice configured[4];
-    if (plan.pair)
-      return c.drop.on ? launch(linear_umma_kernel<ACT, true, true>, configured[3])
-                       : launch(linear_umma_kernel<ACT, false, true>, configured[2]);
-    return c.drop.on ? launch(linear_umma_kernel<ACT, true, false>, configured[1])
-                     : launch(linear_umma_kernel<ACT, false, false>, configured[0]);
+    static PerDevice configured[8];
+    auto by = [&](auto drop, auto res) -> int {
+      constexpr bool DROP = decltype(drop)::value, RES = decltype(res)::value;
+      PerDevice* const d = configured + 2 * (2 * DROP + RES);
+      return plan.pair ? launch(linear_umma_kernel<ACT, DROP, RES, true>, d[1])
+                       : launch(linear_umma_kernel<ACT, DROP, RES, false>, d[0]);
+    };
+    if (c.drop.on)
+      return c.residual != nullptr ? by(std::true_type{}, std::true_type{}) : by(std::true_type{}, std::false_type{});
+    return c.residual != nullptr ? by(std::false_type{}, std::true_type{}) : by(std::false_type{}, std::false_type{});
   });
 }
 

@@ -52,6 +52,8 @@ __device__ __forceinline__ void note_used(const Drop& d) {
 template <int G>
 __device__ __forceinline__ void philox(const Stream& s, const uint64_t (&group)[G], uint32_t (&w)[4 * G]) {
   uint32_t k0 = s.k0, k1 = s.k1;
+  // the round keys are added up here: kept for the next call they would take twenty registers
+  asm volatile("" : "+r"(k0), "+r"(k1));
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     w[4 * g] = static_cast<uint32_t>(group[g]);
@@ -126,6 +128,35 @@ __device__ __forceinline__ float at_most(float x, float hi) {
   return y;
 }
 
+// Two fp32 numbers in a pair of registers: an instruction for both (as long on the FMA pipe, but one issue slot).
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 two(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 two(float a) { return two(a, a); }
+__device__ __forceinline__ void parts(F2 x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v));
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 // 2 sqrt(2/pi) and 0.044715 times that: gelu_tanh(z) = z / (1 + exp(-(A z + B z^3)))
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.071354816272600247f;
@@ -135,17 +166,6 @@ constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.071354816272600247f;
 //   exp(a^2/2) a Phi(-a) = S(t), c = 0.4, off by at most 8.6e-5 (S + 0.002).  With it gelu(z) =
 //       max(z, 0) - |z| Phi(-|z|) needs no case for infinities: t, exp(-a^2/2) and S stay finite.
 //   exp(a^2/2) Phi(-a) = Q(t), c = 0.38, off by at most 3.7e-5 Q.
-__device__ __forceinline__ float tail_times_a(float a, float z) {
-  const float t = rcp(fmaf(0.4f, a, 1.f));
-  const float e = ex2(z * (z * (-0.5f * kLog2e)));
-  float q = 0.2135479748249054f;
-  q = fmaf(q, t, -0.5766780972480774f);
-  q = fmaf(q, t, 0.06343623995780945f);
-  q = fmaf(q, t, -0.10194139182567596f);
-  q = fmaf(q, t, 0.0027213171124458313f);
-  q = fmaf(q, t, 0.3989139497280121f);
-  return q * e;
-}
 __device__ __forceinline__ float tail_poly(float a) {
   const float t = rcp(fmaf(0.38f, a, 1.f));
   float q = -0.0906074270606041f;
@@ -156,36 +176,59 @@ __device__ __forceinline__ float tail_poly(float a) {
   return fmaf(q, t, 1.705829163256567e-05f);
 }
 
-// FAST: for results that are rounded to bf16.
-template <int ACT, bool FAST>
+// For fp32 data.
+template <int ACT>
 __device__ __forceinline__ float act(float z) {
   if constexpr (ACT == LBP_ACT_NONE) {
     return z;
   } else if constexpr (ACT == LBP_ACT_RELU) {
     return at_least(z, 0.f);
   } else if constexpr (ACT == LBP_ACT_GELU) {
-    if constexpr (FAST) {
-      return fmaxf(z, 0.f) - tail_times_a(fabsf(z), z);   // (a NaN comes through the tail)
-    } else {
-      const float c = at_least(z, -100.f);
-      return 0.5f * c * erfcf(c * -0.70710678118654752f);
-    }
+    const float c = at_least(z, -100.f);
+    return 0.5f * c * erfcf(c * -0.70710678118654752f);
   } else if constexpr (ACT == LBP_ACT_GELU_TANH) {
     const float c = at_least(z, -30.f);
-    const float u = c * fmaf(kTanhB, c * c, kTanhA);
-    if constexpr (FAST)
-      return c * rcp(1.f + ex2(-kLog2e * u));
-    else
-      return c / (1.f + expf(-u));
+    return c / (1.f + expf(-c * fmaf(kTanhB, c * c, kTanhA)));
   } else {
     const float c = at_least(z, -100.f);
-    if constexpr (FAST)
-      return c * rcp(1.f + ex2(-kLog2e * c));
-    else
-      return c / (1.f + expf(-c));
+    return c / (1.f + expf(-c));
   }
 }
 
+// For results that are rounded to bf16: of two numbers.
+template <int ACT>
+__device__ __forceinline__ void act_fast(float& z0, float& z1) {
+  if constexpr (ACT == LBP_ACT_RELU) {
+    z0 = at_least(z0, 0.f);
+    z1 = at_least(z1, 0.f);
+  } else if constexpr (ACT == LBP_ACT_GELU) {
+    const F2 t = two(rcp(fmaf(0.4f, fabsf(z0), 1.f)), rcp(fmaf(0.4f, fabsf(z1), 1.f)));
+    const F2 z = two(z0, z1);
+    float e0, e1;
+    parts(mul2(z, mul2(z, two(-0.5f * kLog2e))), e0, e1);
+    F2 q = fma2(t, two(0.2135479748249054f), two(-0.5766780972480774f));
+    q = fma2(q, t, two(0.06343623995780945f));
+    q = fma2(q, t, two(-0.10194139182567596f));
+    q = fma2(q, t, two(0.0027213171124458313f));
+    q = fma2(q, t, two(0.3989139497280121f));
+    // (a NaN comes through the exponential)
+    parts(fma2(q, two(-ex2(e0), -ex2(e1)), two(fmaxf(z0, 0.f), fmaxf(z1, 0.f))), z0, z1);
+  } else if constexpr (ACT == LBP_ACT_GELU_TANH || ACT == LBP_ACT_SILU) {
+    // z / (1 + exp(-u))
+    const F2 c = two(at_least(z0, ACT == LBP_ACT_SILU ? -100.f : -30.f), at_least(z1, ACT == LBP_ACT_SILU ? -100.f : -30.f));
+    F2 u;
+    if constexpr (ACT == LBP_ACT_SILU)
+      u = mul2(c, two(-kLog2e));
+    else
+      u = mul2(c, fma2(mul2(c, c), two(-kLog2e * kTanhB), two(-kLog2e * kTanhA)));
+    float e0, e1;
+    parts(u, e0, e1);
+    parts(add2(two(ex2(e0), ex2(e1)), two(1.f)), e0, e1);
+    parts(mul2(c, two(rcp(e0), rcp(e1))), z0, z1);
+  }
+}
+
+// FAST: for results that are rounded to bf16.
 template <int ACT, bool FAST>
 __device__ __forceinline__ float act_slope(float z) {
   constexpr float kInvSqrt2Pi = 0.3989422804014327f;
