@@ -8,11 +8,16 @@
 // next to one another, so that x comes from HBM once and W stays in L2.
 //
 // Warps: 0 TMA loads, 1 tcgen05, 2-17 the epilogue, four to each quarter of the accumulator's lanes, which
-// take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels.  A
-// thread has a token, so that its channels lie together: one Philox call serves eight of them, and 16 are 32 bytes, a
-// whole sector, which it writes (and reads of the residual) in one instruction.  A warp's 32 rows of 32 bytes move 5.6
-// TB/s from all SMs, rows of 128 bytes by way of shared memory 6.1 (16-byte pieces 1.65, TMA stores of 128-byte
-// rows 3.5); what the way through shared memory costs in instructions is more.
+// take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels, 16 channels at a
+// time.  A thread has a token, so that its channels lie together and one Philox call serves eight of them.  The
+// results go to a box in shared memory and out by TMA, which clips what hangs over the last token and channel; z in a
+// pass of its own ahead of y's, through the same box.  The residual is read 32 bytes (a sector) a thread.
+//
+// What bounds it, at 32768 tokens 768 -> 3072 and 1965 MHz: the operands' way from L2 (1.2 GB: 93 us without any
+// store, 1.66 PFLOP/s), which the stores share (y 22 us, z 27), and with GELU and dropout the epilogue's arithmetic
+// (31 instructions an element with z).  Tried: a 32-byte store a thread (no shared memory, six stages: 112, z
+// 149, all 175 us, 48 -> 192 channels 46 instead of 43), a bulk copy per row by its thread (116 and 201), twelve warps
+// (116, 142, 185).
 #include "layer_math.cuh"
 #include "ptx_sm100.cuh"
 
@@ -23,9 +28,10 @@ namespace {
 
 constexpr int kBM = 128, kBK = 64;
 constexpr int kABytes = kBM * kBK * 2;
-constexpr int kEpilogueWarps = 16, kPerQuarter = kEpilogueWarps / 4;
+constexpr int kPerQuarter = 4, kEpilogueWarps = 4 * kPerQuarter;
 constexpr int kThreads = (2 + kEpilogueWarps) * 32;
-constexpr int kBiasBytes = kEpilogueWarps * 64 * 4;   // a chunk's, for each warp
+constexpr int kBoxBytes = 32 * 128;
+constexpr int kBiasBytes = 2 * kPerQuarter * 64 * 4, kOutBytes = kEpilogueWarps * kBoxBytes;   // bias: of a tile and the next
 constexpr int kMaxStages = 8;
 constexpr int kBarBytes = 256;
 constexpr int kSmemMax = 227 * 1024;
@@ -44,20 +50,19 @@ struct Params {
   uint32_t* status;
 };
 struct Maps {
-  CUtensorMap x, W;
+  CUtensorMap x, W, y, z;
 };
 
-// 16 channels of a row, as far as they go (`n` of them), to and from registers.
-__device__ __forceinline__ void write16(__nv_bfloat16* to, const uint32_t (&w)[8], int n, bool wide) {
-  if (wide && n >= 16) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-  } else {
-    if (n > 0) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-    if (n > 8) *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-  }
+__device__ __forceinline__ void store_2d(const CUtensorMap* m, const void* src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(m)),
+               "r"(ptx::smem_u32(src)), "r"(x), "r"(y)
+               : "memory");
 }
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// 16 channels of a row, as far as they go (`n` of them).
 __device__ __forceinline__ void read16(const __nv_bfloat16* from, uint32_t (&w)[8], int n, bool wide) {
   if (wide && n >= 16) {
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -76,9 +81,9 @@ template <int ACT, bool DROP, bool RES, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_umma_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   constexpr int kCtas = PAIR ? 2 : 1;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  float* const biases = reinterpret_cast<float*>(smem + p.stages * p.stage_bytes);
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t* const outs = smem + p.stages * p.stage_bytes;
+  float* const biases = reinterpret_cast<float*>(outs + kOutBytes);
   uint64_t* const full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(biases) + kBiasBytes);   // [kMaxStages]
   uint64_t* const empty = full + kMaxStages;
   uint64_t* const acc_full = empty + kMaxStages;    // [2]
@@ -205,100 +210,129 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     // =========================== epilogue ===========================
     const int e = warp - 2, quarter = warp & 3;
-    float* const bias = biases + e * 64;
+    uint8_t* const box = outs + e * kBoxBytes;
+    uint8_t* const mine = box + lane * 128;
     const Stream stream = DROP ? open_stream(p.drop) : Stream{};
     if (blockIdx.x == 0 && warp == 2 && lane == 0) note_used(p.drop);
     const int chunks = p.BN / 64;
     bool ok = true;
-    int n = 0;
-    for (int t = unit; t < p.tiles; t += units, ++n) {
-      const int m = t / p.tiles_n, c = ((e >> 2) + n) % kPerQuarter;   // (in turn, where there are fewer chunks than warps)
+    int n = 0, next = e >> 2;   // chunks go round, so that every warp has as many
+    for (int t = unit; t < p.tiles && ok; t += units, ++n) {
+      const int m = t / p.tiles_n;
       const long long row = static_cast<long long>(m * kCtas + rank) * kBM + quarter * 32 + lane;
-      const int col = (t - m * p.tiles_n) * p.BN + c * 64;
-      const int cols = c < chunks ? p.Cout - col : 0;          // of this chunk on
-      const int mine = row < p.rows ? cols : 0;                // ... in this thread's row
-      if (p.bias != nullptr && cols > 0) {
-        const uint32_t w = 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
-        __syncwarp();   // (everyone has read the last chunk's)
-        *reinterpret_cast<float2*>(bias + 2 * lane) = make_float2(bf16_lo(w), bf16_hi(w));
-      }
-      const __nv_bfloat16* const res = p.residual + row * p.pr + col;
-      uint32_t r[8];
-      if constexpr (RES) read16(res, r, mine, p.wide);
-      __syncwarp();
-      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u) &&
-                                       *abort_flag == 0);
-      if (!ok) break;
-      ptx::tc_fence_after_sync();
-      const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols + c * 64;
-      const uint64_t number = static_cast<uint64_t>(p.first + row * p.step + col);
-      __nv_bfloat16 *const y = p.y + row * p.py + col, *const z = p.z + row * p.pz + col;
-
-      // 16 channels at h * 16, from the accumulator in a
-      auto step = [&](int h, const uint32_t (&a)[16]) {
-        float v[16], out[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(a[j]);
-        if (p.bias != nullptr) {
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(bias + h * 16 + j);
-            parts(add2(two(v[j], v[j + 1]), two(b.x, b.y)), v[j], v[j + 1]);
-            parts(add2(two(v[j + 2], v[j + 3]), two(b.z, b.w)), v[j + 2], v[j + 3]);
-          }
-        }
-        const int left = mine - h * 16;
-        uint32_t w[8];
-        if (p.z != nullptr) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
-          write16(z + h * 16, w, left, p.wide);
-        }
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) act_fast<ACT>(v[j], v[j + 1]);
-        if constexpr (RES) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(r[j]), out[2 * j + 1] = bf16_hi(r[j]);
-          if (h < 3) read16(res + (h + 1) * 16, r, left - 16, p.wide);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) out[j] = 0.f;
-        }
-        if constexpr (DROP) {
-          const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
-          philox<2>(stream, group, w);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
-        } else if constexpr (RES) {
-#pragma unroll
-          for (int j = 0; j < 16; j += 2) parts(add2(two(out[j], out[j + 1]), two(v[j], v[j + 1])), out[j], out[j + 1]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) out[j] = v[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(out[2 * j], out[2 * j + 1]);
-        write16(y + h * 16, w, left, p.wide);
+      bool waited = false;
+      auto wait = [&] {
+        waited = true;
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u) &&
+                                         *abort_flag == 0);
+        ptx::tc_fence_after_sync();
       };
-      // a step's accumulator is read while the one before is worked on
-      uint32_t a0[16], a1[16];
-      if (cols > 0) {
-        ptx::tmem_ld_32x16(acc, a0);
-        ptx::tmem_ld_wait();
-      }
+      int c = next;
+      static_assert(kPerQuarter >= 4, "at most one chunk of a tile a warp: the biases of a tile are written once");
+      for (; c < chunks; c += kPerQuarter) {
+        const int col = (t - m * p.tiles_n) * p.BN + c * 64;
+        const int cols = p.Cout - col;                           // of this chunk on
+        const int here = row < p.rows ? cols : 0;                // ... in this thread's row
+        const uint32_t two_biases = p.bias != nullptr && 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
+        const __nv_bfloat16* const res = p.residual + row * p.pr + col;
+        uint32_t r[8];
+        if constexpr (RES) read16(res, r, here, p.wide);
+        if (!waited) wait();
+        if (!ok) break;
+        // The four warps of these columns write the same.  (What is overwritten belongs to the tile before the last,
+        // whose accumulator every warp has released.)
+        float* const bias = biases + ((n & 1) * kPerQuarter + (e >> 2)) * 64;
+        *reinterpret_cast<float2*>(bias + 2 * lane) = make_float2(bf16_lo(two_biases), bf16_hi(two_biases));
+        __syncwarp();
+        const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols + c * 64;
+        const uint64_t number = static_cast<uint64_t>(p.first + row * p.step + col);
+      
+
+        auto put = [&](int h, const float (&o)[16]) {
+          if (h == 0) {
+            if (lane == 0) bulk_wait_read();   // the box has been sent
+            __syncwarp();
+          }
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+            *reinterpret_cast<uint4*>(mine + (((h * 2 + g) ^ (lane & 7)) << 4)) =
+                make_uint4(pack_bf16x2(o[8 * g], o[8 * g + 1]), pack_bf16x2(o[8 * g + 2], o[8 * g + 3]),
+                           pack_bf16x2(o[8 * g + 4], o[8 * g + 5]), pack_bf16x2(o[8 * g + 6], o[8 * g + 7]));
+        };
+        // 16 channels at h * 16, from the accumulator in a
+        auto step = [&](auto is_z, int h, const uint32_t (&a)[16]) {
+          constexpr bool Z = decltype(is_z)::value;
+          float v[16], out[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(a[j]);
+          if (p.bias != nullptr) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(bias + h * 16 + j);
+              parts(add2(two(v[j], v[j + 1]), two(b.x, b.y)), v[j], v[j + 1]);
+              parts(add2(two(v[j + 2], v[j + 3]), two(b.z, b.w)), v[j + 2], v[j + 3]);
+            }
+          }
+          const int left = here - h * 16;
+          uint32_t w[8];
+          if (Z) {
+            put(h, v);
+            return;
+          }
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) act_fast<ACT>(v[j], v[j + 1]);
+          if constexpr (RES) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(r[j]), out[2 * j + 1] = bf16_hi(r[j]);
+            if (h < 3) read16(res + (h + 1) * 16, r, left - 16, p.wide);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) out[j] = 0.f;
+          }
+          if constexpr (DROP) {
+            const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
+            philox<2>(stream, group, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
+          } else if constexpr (RES) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) parts(add2(two(out[j], out[j + 1]), two(v[j], v[j + 1])), out[j], out[j + 1]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) out[j] = v[j];
+          }
+          put(h, out);
+        };
+        // a step's accumulator is read while the one before is worked on
+        auto pass = [&](auto is_z, const CUtensorMap& map) {
+          uint32_t a0[16], a1[16];
+          ptx::tmem_ld_32x16(acc, a0);
+          ptx::tmem_ld_wait();
 #pragma unroll 1
-      for (int h = 0; h < 4 && cols > 0; h += 2) {
-        ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
-        step(h, a0);
-        ptx::tmem_ld_wait();
-        if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
-        step(h + 1, a1);
-        ptx::tmem_ld_wait();
+          for (int h = 0; h < 4 && cols > 0; h += 2) {
+            ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
+            step(is_z, h, a0);
+            ptx::tmem_ld_wait();
+            if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
+            step(is_z, h + 1, a1);
+            ptx::tmem_ld_wait();
+          }
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (cols > 0 && row < p.rows) store_2d(&map, box, col, static_cast<int32_t>(row));
+            bulk_commit();
+          }
+        };
+        if (p.z != nullptr) pass(std::true_type{}, tm.z);
+        pass(std::false_type{}, tm.y);
       }
+      next = c - chunks;
+      if (!waited) wait();
       // the accumulator has been read
       ptx::tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) {
+      if (lane == 0 && ok) {
         if constexpr (PAIR)
           ptx::mbar_arrive_cluster(ptx::map_to_rank(ptx::smem_u32(&acc_empty[n & 1]), 0));
         else
@@ -306,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;
+    bulk_wait_all();   // everything has been written before the CTA leaves
   }
 
   ptx::tc_fence_before_sync();
@@ -375,7 +410,7 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   if (tiles >= (1ll << 31)) return LBP_ERR_SHAPE;
   p.tiles = static_cast<int32_t>(tiles);
   p.stage_bytes = kABytes + part * kBK * 2;
-  const int room = kSmemMax - 1024 - kBarBytes - kBiasBytes;
+  const int room = kSmemMax - kBarBytes - kBiasBytes - kOutBytes;
   p.stages = room / p.stage_bytes < kMaxStages ? room / p.stage_bytes : kMaxStages;
   p.test_stall = g_test_stall ? 1 : 0;
   p.first = c.first;
@@ -389,10 +424,15 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   p.py = c.py;
   p.pz = c.pz;
   auto wide = [](const void* q, int64_t pitch) { return ((reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(2 * pitch)) & 31u) == 0; };
-  p.wide = wide(c.y, c.py) && (c.z == nullptr || wide(c.z, c.pz)) && (c.residual == nullptr || wide(c.residual, c.pr));
+  p.wide = c.residual != nullptr && wide(c.residual, c.pr);
   Maps tm;
   if (int e = encode_matrix_tensor_map(&tm.x, c.x, c.rows, c.Cin, kBM, c.px)) return e;
   if (int e = encode_matrix_tensor_map(&tm.W, c.W, c.Cout, c.Cin, part)) return e;
+  if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py)) return e;
+  tm.z = tm.y;
+  if (c.z != nullptr)
+    if (int e = encode_matrix_tensor_map(&tm.z, c.z, c.rows, c.Cout, 32, c.pz)) return e;
+
   const int units = plan.pair ? sms / 2 : sms;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -404,7 +444,7 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(static_cast<unsigned>(ctas * (tiles < units ? tiles : units)));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = 1024 + p.stages * p.stage_bytes + kBiasBytes + kBarBytes;
+  cfg.dynamicSmemBytes = p.stages * p.stage_bytes + kBiasBytes + kOutBytes + kBarBytes;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = plan.pair ? 2 : 1;
