@@ -47,7 +47,13 @@
 // replaced.  640 x 448 -> 1792, both products: 22 us, with one NaN in g_y 120, with nothing but
 // NaN 141 (FFMA kernel 60 whatever the values; a serial sum per thread from global memory 980
 // and 1120); 2048 x 768 -> 3072: 115, 250 and 803 (436; 1690 and 6850).
+//
+// lbp_linear on fp32 data is a third use, with L = x and C = W, both stored by rows (K contiguous), so that a lane is
+// a token and the sums leave with the epilogue applied: `Out` is layer::LinearCall instead of NoEpilogue.
+#include <type_traits>
+
 #include "gemm_fp32.cuh"
+#include "layer_math.cuh"
 #include "lbp_internal.h"
 #include "ptx_sm100.cuh"
 #include "wht_device.cuh"
@@ -122,8 +128,39 @@ __device__ __forceinline__ uint32_t take_part(float& a, float& b, int part) {
   return w;
 }
 
-// The item of this CTA.
-template <int BN>
+// What happens to the sums: stored, or a layer's epilogue first.
+struct NoEpilogue {};
+template <class Out>
+constexpr bool kLinear = !std::is_same<Out, NoEpilogue>::value;
+// Four channels of a token, from their product.
+__device__ __forceinline__ void emit(const NoEpilogue&, const layer::Stream&, long long, long long, float4) {}
+__device__ __forceinline__ void emit(const layer::LinearCall& p, const layer::Stream& s, long long row, long long ch, float4 sum) {
+  float v[4] = {sum.x, sum.y, sum.z, sum.w}, out[4] = {};
+  auto at = [&](const void* q, int64_t pitch) { return reinterpret_cast<float4*>(static_cast<float*>(const_cast<void*>(q)) + row * pitch + ch); };
+  if (p.bias != nullptr) {
+    const float4 b = *at(p.bias, 0);
+    v[0] += b.x, v[1] += b.y, v[2] += b.z, v[3] += b.w;
+  }
+  if (p.z != nullptr) *at(p.z, p.pz) = make_float4(v[0], v[1], v[2], v[3]);
+#pragma unroll 1
+  for (int pass = 0; pass < (p.act == LBP_ACT_NONE ? 0 : 1); ++pass) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = layer::act_of<false>(p.act, v[j]);
+  }
+  if (p.residual != nullptr) {
+    const float4 r = *at(p.residual, p.pr);
+    out[0] = r.x, out[1] = r.y, out[2] = r.z, out[3] = r.w;
+  }
+  layer::add_dropped(out, v, static_cast<uint64_t>(p.first + row * p.step + ch), s, p.drop);
+  *at(p.y, p.py) = make_float4(out[0], out[1], out[2], out[3]);
+}
+__device__ __forceinline__ layer::Stream stream_of(const NoEpilogue&) { return layer::Stream{}; }
+__device__ __forceinline__ layer::Stream stream_of(const layer::LinearCall& p) {
+  return p.drop.on ? layer::open_stream(p.drop) : layer::Stream{};
+}
+
+// The item of this CTA.  LIN: L is stored by lanes, in shared memory as two boxes of 32 k's in the 128-byte swizzle.
+template <int BN, bool LIN>
 struct Item {
   const CUtensorMap *map_l, *map_c;
   uint8_t *smem, *raw;
@@ -133,6 +170,7 @@ struct Item {
   long long lanes, cols, K;
   int32_t l0, c0, kb0, n_kb;
   bool wt;               // L = B, C = A stored (columns, K), D transposed
+  bool planes;           // K is shared with other items
 
   __device__ __forceinline__ Item(const GemmFp32Jobs& jobs, const Maps& maps) {
     extern __shared__ uint8_t smem_raw[];
@@ -148,7 +186,8 @@ struct Item {
     if (which) t -= jobs.items0;
     const int chunk = t % g.chunks;
     t /= g.chunks;
-    wt = g.a_mn == 0;
+    wt = !LIN && g.a_mn == 0;
+    planes = g.chunks > 1;
     lanes = wt ? g.N : g.M;
     cols = wt ? g.M : g.N;
     K = g.K;
@@ -165,8 +204,14 @@ struct Item {
     uint8_t* const dst = raw + (u & 1) * C::kRaw;
     const int k = (kb0 + (u < n_kb ? u : u - n_kb)) * kBK;
     ptx::mbar_expect_tx(&full[u & 1], C::kRaw);   // boxes count in full, also where they hang over an edge (zeros)
-    ptx::tma_load_2d(dst, map_l, &full[u & 1], l0, k);
-    ptx::tma_load_2d(dst + C::kRawL, map_c, &full[u & 1], wt ? k : c0, wt ? c0 : k);
+    if constexpr (LIN) {
+      ptx::tma_load_2d(dst, map_l, &full[u & 1], k, l0);
+      ptx::tma_load_2d(dst + C::kRawL / 2, map_l, &full[u & 1], k + 32, l0);
+    } else {
+      ptx::tma_load_2d(dst, map_l, &full[u & 1], l0, k);
+    }
+    const bool ck = LIN || wt;   // C is stored by columns
+    ptx::tma_load_2d(dst + C::kRawL, map_c, &full[u & 1], ck ? k : c0, ck ? c0 : k);
   }
   __device__ __forceinline__ bool arrived(int u, uint32_t site) const {
     return ptx::mbar_wait(&full[u & 1], static_cast<uint32_t>(u >> 1) & 1u, status, (7u << 16) | site);
@@ -185,16 +230,17 @@ __device__ __forceinline__ bool stays(float v) {
 // `mine` set.  A thread has kCols / 4 lanes (in runs of four) by 4 columns, which reads less
 // than a lane by kCols.  Not inlined, and with nothing handed over: registers that the kernel
 // spills for this path cost every item of one block 0.5 us.
-template <int BN>
-__device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps& maps, bool few, bool mine) {
+template <int BN, class Out>
+__device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps& maps, const Out& epi, bool few, bool mine) {
   using C = Cfg<BN>;
-  const Item<BN> item(jobs, maps);
+  constexpr bool LIN = kLinear<Out>;
+  const Item<BN, LIN> item(jobs, maps);
   const float* const old = reinterpret_cast<const float*>(item.smem);
   constexpr int kRuns = C::kCols / 16, kAlong = 8 / kRuns;   // runs of a thread; threads along the lanes
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int run = (lane % kAlong) * 4, four = lane / kAlong * 4;
-  const bool wt = item.wt;
-  const int l_at = (warp & 3) * 32 + run, c_at = C::kRawL / 4 + ((warp >> 2) * C::kCols + four) * (wt ? kBK : 1);
+  const bool wt = item.wt, ck = LIN || wt;
+  const int l_at = (warp & 3) * 32 + run, c_at = C::kRawL / 4 + ((warp >> 2) * C::kCols + four) * (ck ? kBK : 1);
   float sum[C::kCols];
 #pragma unroll
   for (int j = 0; j < C::kCols; ++j) sum[j] = 0.f;
@@ -214,11 +260,26 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
         float c[4][4];   // [k][column]
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float4 v = *reinterpret_cast<const float4*>(at + c_at + (wt ? q * kBK + k : (k + q) * BN));
-          if (wt)
+          const float4 v = *reinterpret_cast<const float4*>(at + c_at + (ck ? q * kBK + k : (k + q) * BN));
+          if (ck)
             c[0][q] = v.x, c[1][q] = v.y, c[2][q] = v.z, c[3][q] = v.w;
           else
             c[q][0] = v.x, c[q][1] = v.y, c[q][2] = v.z, c[q][3] = v.w;
+        }
+        if constexpr (LIN) {
+#pragma unroll
+          for (int h = 0; h < kRuns; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int l = l_at + h * 4 * kAlong + i;
+              const float4 v = *reinterpret_cast<const float4*>(at + (k >> 5) * (C::kRawL / 8) + l * 32 + ((((k & 31) >> 2) ^ (l & 7)) << 2));
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float& to = sum[h * 16 + 4 * i + j];
+                to = fmaf(v.w, c[3][j], fmaf(v.z, c[2][j], fmaf(v.y, c[1][j], fmaf(v.x, c[0][j], to))));
+              }
+            }
+          continue;
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -240,6 +301,7 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (warp == kWarps) return;
+  const layer::Stream stream = stream_of(epi);
   const long long l = item.l0 + (warp & 3) * 32 + run, n = item.c0 + (warp >> 2) * C::kCols + four;
 #pragma unroll
   for (int h = 0; h < kRuns; ++h) {
@@ -255,6 +317,25 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
         }
       }
     if (l + h * 4 * kAlong >= item.lanes) continue;
+    if constexpr (LIN) {
+      if (!item.planes) {   // (tokens are any number)
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+          const float4 four_of = i == 0 ? make_float4(v[0][0], v[0][1], v[0][2], v[0][3])
+                                 : i == 1 ? make_float4(v[1][0], v[1][1], v[1][2], v[1][3])
+                                 : i == 2 ? make_float4(v[2][0], v[2][1], v[2][2], v[2][3])
+                                          : make_float4(v[3][0], v[3][1], v[3][2], v[3][3]);
+          const long long row = l + h * 4 * kAlong + i;
+          if (row < item.lanes && n < item.cols) emit(epi, stream, row, n, four_of);
+        }
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (l + h * 4 * kAlong + i < item.lanes && n < item.cols)
+          *reinterpret_cast<float4*>(item.D + (l + h * 4 * kAlong + i) * item.cols + n) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {   // (lanes are a multiple of four, and columns where they lie together)
       if (wt && n + i < item.cols)
@@ -265,22 +346,30 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
   }
 }
 
-template <int BN>
+template <int BN, class Out>
 __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __grid_constant__ GemmFp32Jobs jobs,
-                                                                    const __grid_constant__ Maps maps) {
+                                                                    const __grid_constant__ Maps maps,
+                                                                    const __grid_constant__ Out epi) {
   using C = Cfg<BN>;
-  const Item<BN> item(jobs, maps);
+  constexpr bool LIN = kLinear<Out>;
+  const Item<BN, LIN> item(jobs, maps);
   uint8_t *const smem = item.smem, *const raw = item.raw;
   uint64_t* const full = item.full;
   uint64_t* ready = full + 2;                                        // [2]: a block's parts are written
   uint64_t* done = ready + 2;                                        // [2]: its MMAs have completed
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool wt = item.wt;
+  const bool wt = item.wt, ck = LIN || wt;
   const int n_kb = item.n_kb;
   const bool few = n_kb == 1 && item.K - static_cast<long long>(item.kb0) * kBK <= kFewTerms;
 
   if (threadIdx.x == 0) {
+    if constexpr (LIN) {
+      if (blockIdx.x == 0 && epi.drop.used != nullptr) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        layer::note_used(epi.drop);
+      }
+    }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&full[i], 1);
       ptx::mbar_init(&ready[i], kWarps);
@@ -302,16 +391,16 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 
   if (few) {
     if (threadIdx.x == 0) item.load(0);
-    finish_by_fma<BN>(jobs, maps, true, true);
+    finish_by_fma<BN>(jobs, maps, epi, true, true);
     return;
   }
   // L: a thread has its lane's k's of one half of the block.  C: pieces of four numbers, a
   // warp whole 128-byte lines; row `row` + q * rows of the block, in shared memory `hop` apart.
   const bool is_l = warp < 8;
   const int quarter = warp & 3, tid = threadIdx.x & 255;
-  const int c_row = wt ? tid >> 4 : tid / (BN / 4), c_pc = wt ? tid & 15 : tid % (BN / 4);
-  const int hop = (wt ? 16 : 256 / (BN / 4)) * 128;
-  const int to = (wt ? 0 : (c_pc >> 4) * kChunkBytes) + c_row * 128 + ((((c_pc & 15) >> 1) ^ (c_row & 7)) << 4) + (c_pc & 1) * 8;
+  const int c_row = ck ? tid >> 4 : tid / (BN / 4), c_pc = ck ? tid & 15 : tid % (BN / 4);
+  const int hop = (ck ? 16 : 256 / (BN / 4)) * 128;
+  const int to = (ck ? 0 : (c_pc >> 4) * kChunkBytes) + c_row * 128 + ((((c_pc & 15) >> 1) ^ (c_row & 7)) << 4) + (c_pc & 1) * 8;
 
   float sum[C::kCols];
 #pragma unroll
@@ -337,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
   int begun = 0;   // blocks whose MMAs this thread has issued
   if (warp == kWarps) {
     if (ptx::elect_one()) {
-      const uint32_t idesc = ptx::idesc_bf16(kLanes, BN, false, !wt);
+      const uint32_t idesc = ptx::idesc_bf16(kLanes, BN, false, !ck);
       const int n = jobs.test_stall ? 0 : n_kb;
       int loads = 0;   // blocks fetched
       for (; loads < 2 && loads < n; ++loads) item.load(loads);
@@ -356,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 #pragma unroll
           for (int kk = 0; kk < kBK / 16; ++kk) {
             const uint32_t bp = b + kPc[q] * C::kPart;
-            const uint64_t db = wt ? ptx::smem_desc_sw128(bp + kk * 32, 16, 1024)
+            const uint64_t db = ck ? ptx::smem_desc_sw128(bp + kk * 32, 16, 1024)
                                    : ptx::smem_desc_sw128(bp + kk * 2048, kChunkBytes, 1024);
             const uint32_t al = a + kPl[q] * kPartCols + kk * 8;
             if (kk == 0 && (q == 1 || q == 5))
@@ -384,8 +473,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 #pragma unroll
       for (int h = 0; h < 2; ++h) {   // 16 k's
         float v[16];
+        if constexpr (LIN) {
+          const int l = quarter * 32 + lane;
+          const float* const row = reinterpret_cast<const float*>(raw + s * C::kRaw) + (warp >> 2) * (C::kRawL / 8) + l * 32;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = src[(16 * h + j) * kLanes];
+          for (int j = 0; j < 4; ++j) {
+            const float4 f = *reinterpret_cast<const float4*>(row + (((4 * h + j) ^ (l & 7)) << 2));
+            v[4 * j] = f.x, v[4 * j + 1] = f.y, v[4 * j + 2] = f.z, v[4 * j + 3] = f.w;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = src[(16 * h + j) * kLanes];
+        }
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
           uint32_t w[8];
@@ -436,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 #pragma unroll
         for (int j = 0; j < C::kCols; ++j) reinterpret_cast<float*>(smem)[j * kWarps * 32 + threadIdx.x] = sum[j];
       }
-      finish_by_fma<BN>(jobs, maps, false, __any_sync(0xffffffffu, bad));
+      finish_by_fma<BN>(jobs, maps, epi, false, __any_sync(0xffffffffu, bad));
       return;
     }
     if (begun > 0)
@@ -462,6 +561,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
           make_float4(sum[4 * c], sum[4 * c + 1], sum[4 * c + 2], sum[4 * c + 3]);
     __syncwarp();
     const int c = lane % kRowPieces;
+    if constexpr (LIN) {
+      if (!item.planes) {
+        const layer::Stream stream = stream_of(epi);
+#pragma unroll 1
+        for (int row = lane / kRowPieces; row < 32; row += 32 / kRowPieces) {
+          const long long gm = item.l0 + quarter * 32 + row, gn = n0 + 4 * c;
+          if (gm < lanes && gn < cols) emit(epi, stream, gm, gn, mine[row * kRowPieces + (c ^ (row & (kRowPieces - 1)))]);
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += 32 / kRowPieces) {
       const int row = r0 + lane / kRowPieces;
@@ -477,22 +587,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 static thread_local bool g_test_stall = false;
 void set_test_stall_fp32(bool on) { g_test_stall = on; }
 
-template <int BN>
-static int launch_bn(const GemmFp32Jobs& js, int n, cudaStream_t stream) {
+template <int BN, class Out>
+static int launch_items(const GemmFp32Jobs& js, const split::Maps& maps, const Out& out, cudaStream_t stream) {
   using C = split::Cfg<BN>;
-  split::Maps maps;
-  for (int i = 0; i < n; ++i) {
-    const GemmFp32Job& g = js.j[i];
-    if (g.a_mn) {
-      if (int e = encode_f32_matrix_map(&maps.l[i], g.A, g.K, g.M, split::kBK, split::kLanes)) return e;
-      if (int e = encode_f32_matrix_map(&maps.c[i], g.B, g.K, g.N, split::kBK, BN)) return e;
-    } else {
-      if (int e = encode_f32_matrix_map(&maps.l[i], g.B, g.K, g.N, split::kBK, split::kLanes)) return e;
-      if (int e = encode_f32_matrix_map(&maps.c[i], g.A, g.M, g.K, BN, split::kBK)) return e;
-    }
-  }
   static PerDevice configured;
-  const auto kern = split::gemm_fp32_split_kernel<BN>;
+  const auto kern = split::gemm_fp32_split_kernel<BN, Out>;
   if (int e = allow_dynamic_smem(configured, reinterpret_cast<const void*>(kern), C::kSmem)) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr;
@@ -504,14 +603,123 @@ static int launch_bn(const GemmFp32Jobs& js, int n, cudaStream_t stream) {
   cfg.stream = stream;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, js, maps));
+  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, js, maps, out));
   count_launch();
   return LBP_OK;
+}
+
+template <int BN>
+static int launch_bn(const GemmFp32Jobs& js, int n, cudaStream_t stream) {
+  split::Maps maps;
+  for (int i = 0; i < n; ++i) {
+    const GemmFp32Job& g = js.j[i];
+    if (g.a_mn) {
+      if (int e = encode_f32_matrix_map(&maps.l[i], g.A, g.K, g.M, split::kBK, split::kLanes)) return e;
+      if (int e = encode_f32_matrix_map(&maps.c[i], g.B, g.K, g.N, split::kBK, BN)) return e;
+    } else {
+      if (int e = encode_f32_matrix_map(&maps.l[i], g.B, g.K, g.N, split::kBK, split::kLanes)) return e;
+      if (int e = encode_f32_matrix_map(&maps.c[i], g.A, g.M, g.K, BN, split::kBK)) return e;
+    }
+  }
+  return launch_items<BN>(js, maps, split::NoEpilogue{}, stream);
 }
 
 int launch_gemm_fp32_split(GemmFp32Jobs& js, int n, int bn, cudaStream_t stream) {
   js.test_stall = g_test_stall ? 1 : 0;
   return bn == 64 ? launch_bn<64>(js, n, stream) : launch_bn<128>(js, n, stream);
 }
+
+// ---- lbp_linear on fp32 data ----
+namespace layer {
+
+namespace {
+
+// The planes of a K in pieces, added up in order, and the epilogue.
+__global__ void __launch_bounds__(256) linear_finish_kernel(const float* planes, int chunks, const __grid_constant__ LinearCall p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Stream s = p.drop.on ? open_stream(p.drop) : Stream{};
+  const int per_row = p.Cout / 4;
+  const long long n = p.rows * per_row, plane = p.rows * p.Cout;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+    const long long row = i < (1ll << 31) ? static_cast<int>(i) / per_row : i / per_row;
+    float4 sum = *reinterpret_cast<const float4*>(planes + 4 * i);
+    for (int c = 1; c < chunks; ++c) {
+      const float4 v = *reinterpret_cast<const float4*>(planes + c * plane + 4 * i);
+      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+    split::emit(p, s, row, 4 * (i - row * per_row), sum);
+  }
+}
+
+// How a product is cut: columns of a tile, k-blocks of an item.  The times are those of the form table in gemm_fp32.cu.
+struct Cut {
+  int bn, chunks;
+};
+Cut cut(long long rows, int Cin, int Cout) {
+  const long long kb = (Cin + split::kBK - 1) / split::kBK;
+  Cut best{64, 1};
+  double least = -1.0;
+  for (int bn : {64, 128}) {
+    const long long tiles = ((rows + split::kLanes - 1) / split::kLanes) * ((Cout + bn - 1) / bn);
+    for (long long chunks = 1; chunks <= kb && chunks <= 16; ++chunks) {
+      const long long per = (kb + chunks - 1) / chunks;
+      if ((kb + per - 1) / per != chunks) continue;
+      const double planes = chunks > 1 ? static_cast<double>(chunks) * rows * Cout * 4.0 : 0.0;
+      if (planes > 48e6) continue;
+      double t = static_cast<double>((tiles * chunks + 147) / 148) * (bn == 64 ? per * 1.05 + 2.5 : per * 1.45 + 3.5);
+      if (chunks > 1) t += 2.5 + 2.0 * planes / 8e6;
+      if (least < 0.0 || t < least) {
+        least = t;
+        best = Cut{bn, static_cast<int>(chunks)};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace
+
+size_t linear_fp32_scratch_bytes(long long rows, int Cin, int Cout) {
+  const Cut c = cut(rows, Cin, Cout);
+  return c.chunks > 1 ? static_cast<size_t>(c.chunks) * rows * Cout * 4 : 0;
+}
+
+int launch_linear_fp32(const LinearCall& c, cudaStream_t stream) {
+  Cut how = cut(c.rows, c.Cin, c.Cout);
+  if (how.chunks > 1 && static_cast<size_t>(how.chunks) * c.rows * c.Cout * 4 > c.scratch_bytes) how.chunks = 1;
+  const long long tiles_c = (c.Cout + how.bn - 1) / how.bn, tiles = (c.rows + split::kLanes - 1) / split::kLanes * tiles_c;
+  const int kb = (c.Cin + split::kBK - 1) / split::kBK;
+  if (tiles * how.chunks >= (1ll << 31)) return LBP_ERR_SHAPE;
+  GemmFp32Jobs js{};
+  float* const planes = static_cast<float*>(c.scratch);
+  js.j[0] = GemmFp32Job{static_cast<const float*>(c.x), static_cast<const float*>(c.W), how.chunks > 1 ? planes : static_cast<float*>(c.y),
+                        c.rows, c.Cout, c.Cin, 0, static_cast<int32_t>(tiles_c), static_cast<int32_t>(tiles), kb,
+                        (kb + how.chunks - 1) / how.chunks, how.chunks};
+  js.items0 = js.items = static_cast<int32_t>(tiles * how.chunks);
+  js.status = c.status;
+  js.test_stall = g_test_stall ? 1 : 0;
+  split::Maps maps;
+  if (int e = encode_f32_matrix_map(&maps.l[0], c.x, c.rows, c.Cin, split::kLanes, 32, c.px, true)) return e;
+  if (int e = encode_f32_matrix_map(&maps.c[0], c.W, c.Cout, c.Cin, how.bn, split::kBK)) return e;
+  maps.l[1] = maps.l[0];
+  maps.c[1] = maps.c[0];
+  if (int e = how.bn == 64 ? launch_items<64>(js, maps, c, stream) : launch_items<128>(js, maps, c, stream)) return e;
+  if (how.chunks == 1) return LBP_OK;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  const long long blocks = (c.rows * (c.Cout / 4) + 255) / 256;
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks < 148 * 8 ? blocks : 148 * 8));
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_finish_kernel, static_cast<const float*>(planes), how.chunks, c));
+  count_launch();
+  return LBP_OK;
+}
+
+}  // namespace layer
 
 }  // namespace lbp

@@ -173,7 +173,7 @@ extern "C" {
 
 size_t lbp_linear_workspace_bytes(long long rows, int Cin, int Cout, int dtype) {
   if (check_rows(rows, Cin, dtype) != LBP_OK || check_rows(rows, Cout, dtype) != LBP_OK) return 0;
-  return kStatusBytes;
+  return kStatusBytes + linear_scratch_bytes(rows, Cin, Cout, dtype);
 }
 
 int lbp_linear(const void* x, const void* W, const void* bias, const void* residual, void* y, void* z,

@@ -228,6 +228,28 @@ __device__ __forceinline__ void act_fast(float& z0, float& z1) {
   }
 }
 
+// The activation of a call, one element at a time.
+template <bool FAST, int ACT>
+__device__ __forceinline__ float act_one(float z) {
+  if constexpr (FAST) {
+    float other = 0.f;
+    act_fast<ACT>(z, other);
+    return z;
+  } else {
+    return act<ACT>(z);
+  }
+}
+template <bool FAST>
+__device__ __forceinline__ float act_of(int a, float z) {
+  switch (a) {
+    case LBP_ACT_RELU: return act_one<FAST, LBP_ACT_RELU>(z);
+    case LBP_ACT_GELU: return act_one<FAST, LBP_ACT_GELU>(z);
+    case LBP_ACT_GELU_TANH: return act_one<FAST, LBP_ACT_GELU_TANH>(z);
+    case LBP_ACT_SILU: return act_one<FAST, LBP_ACT_SILU>(z);
+  }
+  return z;
+}
+
 // FAST: for results that are rounded to bf16.
 template <int ACT, bool FAST>
 __device__ __forceinline__ float act_slope(float z) {
@@ -320,6 +342,10 @@ struct LinearCall {
 };
 int launch_linear(const LinearCall& c, cudaStream_t stream);
 int launch_linear_umma(const LinearCall& c, cudaStream_t stream);   // bf16
+int launch_linear_fp32(const LinearCall& c, cudaStream_t stream);   // (gemm_fp32_split.cu)
+// Scratch that a call takes.
+size_t linear_scratch_bytes(long long rows, int Cin, int Cout, int dtype);
+size_t linear_fp32_scratch_bytes(long long rows, int Cin, int Cout);
 
 // out = residual + drop(a) act'(z) on the tokens of a grid (rows: H = W = 1).  At most one of z and
 // residual.

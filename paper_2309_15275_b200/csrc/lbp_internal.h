@@ -120,9 +120,10 @@ inline bool is_dense(const lbp_view* v) { return v == nullptr || v->token == 0; 
 int encode_matrix_tensor_map(CUtensorMap* map, const void* base, long long rows, long long cols,
                              int box_rows, long long pitch = 0);
 
-// 2-D row-major fp32 matrix (rows, cols), no swizzle.
+// 2-D row-major fp32 matrix (rows, cols), no swizzle, or the 128-byte one (boxes of 32 columns).  pitch: elements
+// between rows (0: dense).
 int encode_f32_matrix_map(CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows,
-                          int box_cols);
+                          int box_cols, long long pitch = 0, bool swizzle128 = false);
 
 // ---- kernel launchers (each returns an lbp_status) ------------------------
 // Row q of block blk of a projected tensor is row blk * r + q.
