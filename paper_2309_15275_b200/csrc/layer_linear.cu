@@ -2,7 +2,7 @@
 //
 // Few tokens read W once and do next to no arithmetic, so what counts is that every SM has its part of W under way
 // at once and that one launch does it all.
-//   bf16, up to 32 tokens: a CTA has 16 output channels; its warps take turns on K in steps of 32.  W goes from
+//   bf16, up to 16 tokens: a CTA has 16 output channels; its warps take turns on K in steps of 32.  W goes from
 //     memory to the registers of mma.sync as its A operand, 16 bytes a lane (lane l: row l / 4 and row l / 4 + 8, k's
 //     8 (l % 4) on; the k's of an instruction may come in any order as long as x, the B operand, has the
 //     same), so nothing is staged and the tokens cost instructions, not traffic.  The warps' sums meet in shared
@@ -16,8 +16,6 @@ namespace lbp {
 namespace layer {
 
 namespace {
-
-constexpr int kMostTokens = 32;
 
 // One element's epilogue, from its product.
 template <class T>
@@ -47,12 +45,14 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// TT: groups of eight tokens
+// TT: groups of eight tokens; 2^log2_s: CTAs of a cluster, which share K
 template <int TT>
-__global__ void __launch_bounds__(512) linear_rows_bf16_kernel(const __grid_constant__ LinearCall p) {
+__global__ void __launch_bounds__(512) linear_rows_bf16_kernel(const __grid_constant__ LinearCall p, int log2_s) {
   __shared__ float sums[16][16][8 * TT + 1];   // [warp][channel][token]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int ch0 = blockIdx.x * 16, r = lane >> 2, c = (lane & 3) * 8;
+  const int S = 1 << log2_s, rank = blockIdx.x & (S - 1), group = blockIdx.x >> log2_s;
+  const int ch0 = group * 16, r = lane >> 2, c = (lane & 3) * 8;
+  const int per = (((p.Cin + 31) / 32 + S - 1) >> log2_s) * 32, k_from = rank * per, k_to = k_from + per < p.Cin ? k_from + per : p.Cin;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const __nv_bfloat16* const W = static_cast<const __nv_bfloat16*>(p.W);
@@ -61,12 +61,12 @@ __global__ void __launch_bounds__(512) linear_rows_bf16_kernel(const __grid_cons
   float d[TT][4] = {};
   const uint4 none = make_uint4(0u, 0u, 0u, 0u);
   constexpr int U = 4;   // steps under way
-  for (int k0 = warp * 32; k0 < p.Cin; k0 += warps * 32 * U) {
+  for (int k0 = k_from + warp * 32; k0 < k_to; k0 += warps * 32 * U) {
     uint4 a[U][2], b[U][TT];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + u * warps * 32 + c;
-      const bool in = k < p.Cin;
+      const bool in = k < k_to;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         a[u][h] = in && have[h] ? *reinterpret_cast<const uint4*>(W + static_cast<long long>(ch0 + r + 8 * h) * p.Cin + k) : none;
@@ -89,13 +89,33 @@ __global__ void __launch_bounds__(512) linear_rows_bf16_kernel(const __grid_cons
   __syncthreads();
   const Stream s = p.drop.on ? open_stream(p.drop) : Stream{};
   if (blockIdx.x == 0 && threadIdx.x == 0) note_used(p.drop);
-  for (int e = threadIdx.x; e < 16 * static_cast<int>(p.rows); e += blockDim.x) {
-    const int ch = e & 15, token = e >> 4;
-    if (ch0 + ch >= p.Cout) continue;
+  const int outs = 16 * static_cast<int>(p.rows);
+  auto sum_of = [&](int e) {
     float v = 0.f;
-    for (int w = 0; w < warps; ++w) v += sums[w][ch][token];
-    finish_one<__nv_bfloat16>(p, s, token, ch0 + ch, v);
+    for (int w = 0; w < warps; ++w) v += sums[w][e & 15][e >> 4];
+    return v;
+  };
+  auto finish = [&](int e, float v) {
+    if (ch0 + (e & 15) < p.Cout) finish_one<__nv_bfloat16>(p, s, e >> 4, ch0 + (e & 15), v);
+  };
+  if (S == 1) {
+    for (int e = threadIdx.x; e < outs; e += blockDim.x) finish(e, sum_of(e));
+    return;
   }
+  // the CTAs' sums, in the order of their ranks, each output by one of them
+  __shared__ float part[16 * 8 * TT];
+  for (int e = threadIdx.x; e < outs; e += blockDim.x) part[e] = sum_of(e);
+  ptx::cluster_sync_all();
+  for (int e = rank * blockDim.x + threadIdx.x; e < outs; e += S * blockDim.x) {
+    float v = 0.f;
+    for (int q = 0; q < S; ++q) {
+      float f;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(ptx::map_to_rank(ptx::smem_u32(part + e), q)) : "memory");
+      v += f;
+    }
+    finish(e, v);
+  }
+  ptx::cluster_sync_all();   // no CTA leaves while another may still read its sums
 }
 
 __global__ void __launch_bounds__(256) linear_rows_fp32_kernel(const __grid_constant__ LinearCall p) {
@@ -142,40 +162,50 @@ __global__ void __launch_bounds__(256) linear_rows_fp32_kernel(const __grid_cons
   finish_one<float>(p, s, t0 + t, ch0 + (lane >> 3), v[0]);
 }
 
-template <class Kernel>
-int launch(Kernel kernel, dim3 grid, int threads, const LinearCall& c, cudaStream_t stream) {
+template <class Kernel, class... More>
+int launch(Kernel kernel, dim3 grid, int threads, int cluster, cudaStream_t stream, More... more) {
   cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.stream = stream;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, c));
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, more...));
   count_launch();
   return LBP_OK;
 }
 
 int launch_rows(const LinearCall& c, cudaStream_t stream) {
-  if (c.dtype == LBP_F32) return launch(linear_rows_fp32_kernel, dim3((c.Cout + 15) / 16, (c.rows + 7) / 8), 256, c, stream);
-  const int steps = (c.Cin + 31) / 32, warps = steps < 4 ? 4 : steps < 16 ? steps : 16;
-  const dim3 grid((c.Cout + 15) / 16);
-  if (c.rows <= 8) return launch(linear_rows_bf16_kernel<1>, grid, warps * 32, c, stream);
-  if (c.rows <= 16) return launch(linear_rows_bf16_kernel<2>, grid, warps * 32, c, stream);
-  return launch(linear_rows_bf16_kernel<4>, grid, warps * 32, c, stream);
+  if (c.dtype == LBP_F32)
+    return launch(linear_rows_fp32_kernel, dim3((c.Cout + 15) / 16, (c.rows + 7) / 8), 256, 1, stream, c);
+  // CTAs for all SMs, as long as each has 256 k's and more; a warp for every 32 of them
+  const int groups = (c.Cout + 15) / 16;
+  int log2_s = 0;
+  while (log2_s < 3 && (groups << (log2_s + 1)) <= 296 && (c.Cin >> (log2_s + 1)) >= 256) ++log2_s;
+  const int S = 1 << log2_s, steps = ((c.Cin + 31) / 32 + S - 1) / S, warps = steps < 4 ? 4 : steps < 16 ? steps : 16;
+  if (c.rows <= 8) return launch(linear_rows_bf16_kernel<1>, dim3(groups * S), warps * 32, S, stream, c, log2_s);
+  return launch(linear_rows_bf16_kernel<2>, dim3(groups * S), warps * 32, S, stream, c, log2_s);
 }
+
+// Tokens that count as few.
+int few_tokens(int dtype) { return dtype == LBP_F32 ? 32 : 16; }
 
 }  // namespace
 
 size_t linear_scratch_bytes(long long rows, int Cin, int Cout, int dtype) {
-  if (rows <= kMostTokens) return 0;
+  if (rows <= few_tokens(dtype)) return 0;
   return dtype == LBP_F32 ? linear_fp32_scratch_bytes(rows, Cin, Cout) : 0;
 }
 
 int launch_linear(const LinearCall& c, cudaStream_t stream) {
-  if (c.rows <= kMostTokens) return launch_rows(c, stream);
+  if (c.rows <= few_tokens(c.dtype)) return launch_rows(c, stream);
   // coordinates of a tensor map are 32 bits wide
   constexpr long long kMostRows = 1ll << 30;
   LinearCall part = c;

@@ -59,10 +59,20 @@ __device__ __forceinline__ void store_2d(const CUtensorMap* m, const void* src, 
                "r"(ptx::smem_u32(src)), "r"(x), "r"(y)
                : "memory");
 }
+// 16 channels of a row, as far as they go (`n` of them).
+__device__ __forceinline__ void write16(__nv_bfloat16* to, const uint32_t (&w)[8], int n, bool wide) {
+  if (wide && n >= 16) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    if (n > 0) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (n > 8) *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-// 16 channels of a row, as far as they go (`n` of them).
 __device__ __forceinline__ void read16(const __nv_bfloat16* from, uint32_t (&w)[8], int n, bool wide) {
   if (wide && n >= 16) {
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -355,15 +365,199 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// ---- few tiles: K shared among the CTAs of a cluster ----
+//
+// Where the tiles leave SMs without one, the S CTAs of a cluster take a tile together, each a run of its k-blocks.  Their
+// accumulators go to shared memory, and after a cluster barrier CTA r adds up, in the order of the ranks, its share of
+// the columns, 16 at a time, from all of them (distributed shared memory) and runs the epilogue on those: one launch,
+// no planes, sums in a fixed order.  An SM gets 60 bytes a cycle of operands, so what counts is a CTA's bytes, and
+// tiles of 128 columns with more CTAs to a tile beat 64 (1024 tokens 3072 -> 768: 12.4 us unshared).
+constexpr int kSplitStages = 6;
+constexpr int kSplitThreads = 10 * 32;
+constexpr int kSplitSmem = kSplitStages * (kABytes + 128 * kBK * 2) + kBarBytes;
+static_assert(kBM * 128 * 4 <= kSplitStages * kABytes, "the sums take the operands' place");
+
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int ACT, bool DROP, int S>
+__global__ void __launch_bounds__(kSplitThreads, 1)
+    linear_split_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int stage_bytes = p.stage_bytes, BN = p.BN;
+  uint64_t* const full = reinterpret_cast<uint64_t*>(smem + kSplitStages * stage_bytes);
+  uint64_t* const empty = full + kSplitStages;
+  uint64_t* const acc_full = empty + kSplitStages;
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(ptx::cluster_ctarank()), tile = blockIdx.x / S;
+  const int m = tile / p.tiles_n, col0 = (tile - m * p.tiles_n) * BN;
+  const int per = (p.num_kb + S - 1) / S, kb0 = rank * per, kb1 = kb0 + per < p.num_kb ? kb0 + per : p.num_kb;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSplitStages; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    ptx::mbar_init(acc_full, 1);
+    ptx::mbar_fence_init();
+    ptx::prefetch_tensormap(&tm.x);
+    ptx::prefetch_tensormap(&tm.W);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(tmem_slot, BN);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+      const uint64_t keep = ptx::l2_policy_evict_last();
+      for (int kb = kb0, i = 0; kb < kb1 && !p.test_stall; ++kb, ++i) {
+        const int s = i % kSplitStages;
+        if (!ptx::mbar_wait(&empty[s], ((i / kSplitStages) + 1) & 1u, p.status, kSite | 7u)) break;
+        uint8_t* const sa = smem + s * stage_bytes;
+        ptx::mbar_expect_tx(&full[s], stage_bytes);
+        ptx::tma_load_2d_hint(sa, &tm.x, &full[s], kb * kBK, m * kBM, keep);
+        ptx::tma_load_2d_hint(sa + kABytes, &tm.W, &full[s], kb * kBK, col0, keep);
+      }
+    }
+  } else if (warp == 1) {
+    if (ptx::elect_one()) {
+      const uint32_t idesc = ptx::idesc_bf16(kBM, BN, false, false);
+      bool ok = true;
+      for (int kb = kb0, i = 0; kb < kb1 && ok; ++kb, ++i) {
+        const int s = i % kSplitStages;
+        ok = ptx::mbar_wait(&full[s], (i / kSplitStages) & 1u, p.status, kSite | 8u);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        const uint32_t sa = ptx::smem_u32(smem + s * stage_bytes), sb = sa + kABytes;
+#pragma unroll
+        for (int kk = 0; kk < kBK / 16; ++kk)
+          ptx::mma_bf16_ss(tmem_base, ptx::smem_desc_sw128(sa + kk * 32, 16, 1024), ptx::smem_desc_sw128(sb + kk * 32, 16, 1024),
+                           idesc, (i == 0 && kk == 0) ? 0u : 1u);
+        ptx::mma_commit(&empty[s]);
+      }
+      if (ok) ptx::mma_commit(acc_full);
+    }
+  }
+  const int quarter = warp & 3, row = quarter * 32 + lane, half = (warp - 2) >> 2;   // warps 2-9: a row of the tile a thread, every other 16 columns
+  float* const part = reinterpret_cast<float*>(smem);        // four columns of a row at ((column / 4) * 128 + row) * 4
+  if (warp >= 2) {
+    // (a CTA without k-blocks, where they do not share out evenly, has zeros)
+    bool ok = kb0 < kb1;
+    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(acc_full, 0, p.status, kSite | 9u));
+    ptx::tc_fence_after_sync();
+#pragma unroll 1
+    for (int c = half * 16; c < BN; c += 32) {
+      uint32_t a[16];
+      if (ok) {
+        ptx::tmem_ld_32x16(tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + c, a);
+        ptx::tmem_ld_wait();
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] = 0u;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint4*>(part + ((c / 4 + j) * kBM + row) * 4) = make_uint4(a[4 * j], a[4 * j + 1], a[4 * j + 2], a[4 * j + 3]);
+    }
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::cluster_sync_all();
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem_base, BN);
+  }
+  if (warp >= 2) {
+    const Stream stream = DROP ? open_stream(p.drop) : Stream{};
+    if (blockIdx.x == 0 && threadIdx.x == 64) note_used(p.drop);
+    const long long grow = static_cast<long long>(m) * kBM + row;
+    const int steps = BN / 16, to = (rank + 1) * steps / S * 16;
+#pragma unroll 1
+    for (int c = (rank * steps / S + half) * 16; c < to; c += 32) {
+      const int col = col0 + c, left = grow < p.rows ? p.Cout - col : 0;
+      float v[16], out[16];
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) out[j] = 0.f;
+      if (p.residual != nullptr) {
+        read16(p.residual + grow * p.pr + col, w, left, p.wide);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(w[j]), out[2 * j + 1] = bf16_hi(w[j]);
+      }
+      // (all of them asked for before the first is used)
+      float4 f[S][4];
+#pragma unroll
+      for (int q = 0; q < S; ++q) {
+        const uint32_t from = ptx::map_to_rank(ptx::smem_u32(part + ((c / 4) * kBM + row) * 4), q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[q][j] = ld_cluster(from + j * kBM * 16);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int q = 1; q < S; ++q) f[0][j].x += f[q][j].x, f[0][j].y += f[q][j].y, f[0][j].z += f[q][j].z, f[0][j].w += f[q][j].w;
+        v[4 * j] = f[0][j].x, v[4 * j + 1] = f[0][j].y, v[4 * j + 2] = f[0][j].z, v[4 * j + 3] = f[0][j].w;
+      }
+      if (left <= 0) continue;
+      if (p.bias != nullptr) {
+        float b[8];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (left <= g * 8) break;
+          Vec<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(p.bias + col + g * 8)), b);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[g * 8 + j] += b[j];
+        }
+      }
+      if (p.z != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+        write16(p.z + grow * p.pz + col, w, left, p.wide);
+      }
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) act_fast<ACT>(v[j], v[j + 1]);
+      if constexpr (DROP) {
+        const uint64_t g0 = static_cast<uint64_t>(p.first + grow * p.step + col) >> 3, group[2] = {g0, g0 + 1};
+        philox<2>(stream, group, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) out[j] += v[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(out[2 * j], out[2 * j + 1]);
+      write16(p.y + grow * p.py + col, w, left, p.wide);
+    }
+  }
+  ptx::cluster_sync_all();   // no CTA leaves while another may still read its sums
+}
+
 // How a product is cut.
 struct Plan {
   bool pair;
-  int BN;
+  int BN, split;   // split > 1: K shared among so many CTAs
 };
+
+// Cycles of an SM for the epilogue of 128 tokens by bn channels.
+double epilogue_cycles(const LinearCall& c, int bn) {
+  return bn * (10.0 + (c.act != LBP_ACT_NONE ? 16.0 : 0.0) + (c.drop.on ? 12.0 : 0.0)) + 500.0;
+}
 
 Plan choose_plan(const LinearCall& c, int sms) {
   const int num_kb = (c.Cin + kBK - 1) / kBK;
-  Plan best{false, 64};
+  Plan best{false, 64, 1};
   double least = -1.0;
   for (int pair = 0; pair < 2; ++pair) {
     if (pair && (c.rows <= kBM || sms < 2)) continue;
@@ -375,14 +569,28 @@ Plan choose_plan(const LinearCall& c, int sms) {
       // cycles of an SM: a k-block's products and operands (60 bytes a cycle), an element's epilogue
       const double mma = 2.0 * bn, load = (kABytes + (pair ? bn / 2 : bn) * kBK * 2) / 60.0;
       const double main = num_kb * (mma > load ? mma : load) + 200.0;
-      double per = 10.0;
-      if (c.act != LBP_ACT_NONE) per += 16.0;
-      if (c.drop.on) per += 12.0;
-      const double epi = bn * per + 500.0;
+      const double epi = epilogue_cycles(c, bn);
       const double cost = rounds * (main > epi ? main : epi) + (main > epi ? epi : main) + 1500.0;
       if (least < 0.0 || cost < least) {
         least = cost;
-        best = Plan{pair != 0, bn};
+        best = Plan{pair != 0, bn, 1};
+      }
+    }
+  }
+  // K shared: one round, for the price of the exchange (fitted to 3072 -> 768 and 768 -> 768 channels at 33 to 1024
+  // tokens, us unshared / shared: 11.2 / 6.3 and 5.5 / 4.5 at 64, 11.7 / 8.2 and 6.0 / 6.5 at 300, 12.4 / 10.4 at 1024; 768 -> 3072
+  // at 64: 5.6 / 7.0).  Clusters that are resident at once, at a CTA to an SM: 74 of two and 33 of four on the GPU at
+  // hand; others have GPCs of other sizes.
+  constexpr int kClusters[5] = {0, 0, 72, 0, 30};
+  for (int bn = 64; bn <= 128; bn += 64) {
+    if (bn > 64 && c.Cout <= 64) continue;
+    const long long tiles = ((c.rows + kBM - 1) / kBM) * ((c.Cout + bn - 1) / bn);
+    for (int S = 2; S <= 4; S *= 2) {
+      if (tiles > kClusters[S] || S > num_kb) continue;
+      const double cost = (num_kb + S - 1) / S * ((kABytes + bn * kBK * 2) / 60.0) + (S == 2 ? 7000.0 : bn == 64 ? 4600.0 : 8000.0);
+      if (cost < least) {
+        least = cost;
+        best = Plan{false, bn, S};
       }
     }
   }
@@ -424,13 +632,15 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   p.py = c.py;
   p.pz = c.pz;
   auto wide = [](const void* q, int64_t pitch) { return ((reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(2 * pitch)) & 31u) == 0; };
-  p.wide = c.residual != nullptr && wide(c.residual, c.pr);
+  p.wide = c.residual == nullptr || wide(c.residual, c.pr);
+  if (plan.split > 1) p.wide = p.wide && wide(c.y, c.py) && (c.z == nullptr || wide(c.z, c.pz));
   Maps tm;
   if (int e = encode_matrix_tensor_map(&tm.x, c.x, c.rows, c.Cin, kBM, c.px)) return e;
   if (int e = encode_matrix_tensor_map(&tm.W, c.W, c.Cout, c.Cin, part)) return e;
-  if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py)) return e;
-  tm.z = tm.y;
-  if (c.z != nullptr)
+  tm.y = tm.z = tm.x;
+  if (plan.split == 1)   // (else by plain stores)
+    if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py)) return e;
+  if (plan.split == 1 && c.z != nullptr)
     if (int e = encode_matrix_tensor_map(&tm.z, c.z, c.rows, c.Cout, 32, c.pz)) return e;
 
   const int units = plan.pair ? sms / 2 : sms;
@@ -439,7 +649,7 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.x = plan.split > 1 ? plan.split : 2;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(static_cast<unsigned>(ctas * (tiles < units ? tiles : units)));
@@ -447,7 +657,12 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   cfg.dynamicSmemBytes = p.stages * p.stage_bytes + kBiasBytes + kOutBytes + kBarBytes;
   cfg.stream = stream;
   cfg.attrs = attr;
-  cfg.numAttrs = plan.pair ? 2 : 1;
+  cfg.numAttrs = plan.pair || plan.split > 1 ? 2 : 1;
+  if (plan.split > 1) {
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles) * plan.split);
+    cfg.blockDim = dim3(kSplitThreads);
+    cfg.dynamicSmemBytes = kSplitSmem;
+  }
   return with_act(c.act, [&](auto a) -> int {
     constexpr int ACT = decltype(a)::value;
     auto launch = [&](auto kern, PerDevice& configured) -> int {
@@ -456,6 +671,14 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
       count_launch();
       return LBP_OK;
     };
+    if (plan.split > 1) {
+      static PerDevice split_configured[4];
+      if (plan.split == 2)
+        return c.drop.on ? launch(linear_split_kernel<ACT, true, 2>, split_configured[1])
+                         : launch(linear_split_kernel<ACT, false, 2>, split_configured[0]);
+      return c.drop.on ? launch(linear_split_kernel<ACT, true, 4>, split_configured[3])
+                       : launch(linear_split_kernel<ACT, false, 4>, split_configured[2]);
+    }
     static PerDevice configured[8];
     auto by = [&](auto drop, auto res) -> int {
       constexpr bool DROP = decltype(drop)::value, RES = decltype(res)::value;
