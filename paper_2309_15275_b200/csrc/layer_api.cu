@@ -54,6 +54,9 @@ static Drop drop_of(const lbp_epilogue& e) {
   d.used = e.used;
   d.on = t > 0;
   d.above = static_cast<uint32_t>(static_cast<uint64_t>(t > 0 ? t : 1) * 65536u - 1u);
+  // (t = 2^16: a bound that no half reaches)
+  d.low15 = t < 65536 ? static_cast<uint32_t>(t & 0x7fff) * 0x10001u : 0x80008000u;
+  d.low_half = t < 32768 ? 0x80008000u : 0u;
   d.scale = t < 65536 ? static_cast<float>(65536.0 / static_cast<double>(65536 - t)) : 0.f;
   return d;
 }

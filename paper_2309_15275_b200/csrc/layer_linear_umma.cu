@@ -256,9 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols + c * 64;
         const uint64_t number = static_cast<uint64_t>(p.first + row * p.step + col);
-      
-
-        auto put = [&](int h, const float (&o)[16]) {
+        auto put_words = [&](int h, const uint32_t (&w)[8]) {
           if (h == 0) {
             if (lane == 0) bulk_wait_read();   // the box has been sent
             __syncwarp();
@@ -266,8 +264,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int g = 0; g < 2; ++g)
             *reinterpret_cast<uint4*>(mine + (((h * 2 + g) ^ (lane & 7)) << 4)) =
-                make_uint4(pack_bf16x2(o[8 * g], o[8 * g + 1]), pack_bf16x2(o[8 * g + 2], o[8 * g + 3]),
-                           pack_bf16x2(o[8 * g + 4], o[8 * g + 5]), pack_bf16x2(o[8 * g + 6], o[8 * g + 7]));
+                make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+        };
+        auto put = [&](int h, const float (&o)[16]) {
+          uint32_t w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(o[2 * j], o[2 * j + 1]);
+          put_words(h, w);
         };
         // 16 channels at h * 16, from the accumulator in a
         auto step = [&](auto is_z, int h, const uint32_t (&a)[16]) {
@@ -275,13 +278,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           float v[16], out[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(a[j]);
-          if (p.bias != nullptr) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-              const float4 b = *reinterpret_cast<const float4*>(bias + h * 16 + j);
-              parts(add2(two(v[j], v[j + 1]), two(b.x, b.y)), v[j], v[j + 1]);
-              parts(add2(two(v[j + 2], v[j + 3]), two(b.z, b.w)), v[j + 2], v[j + 3]);
-            }
+          for (int j = 0; j < 16; j += 4) {   // (zeros without a bias)
+            const float4 b = *reinterpret_cast<const float4*>(bias + h * 16 + j);
+            parts(add2(two(v[j], v[j + 1]), two(b.x, b.y)), v[j], v[j + 1]);
+            parts(add2(two(v[j + 2], v[j + 3]), two(b.z, b.w)), v[j + 2], v[j + 3]);
           }
           const int left = here - h * 16;
           uint32_t w[8];
@@ -295,11 +296,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(r[j]), out[2 * j + 1] = bf16_hi(r[j]);
             if (h < 3) read16(res + (h + 1) * 16, r, left - 16, p.wide);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) out[j] = 0.f;
           }
-          if constexpr (DROP) {
+          if constexpr (DROP && !RES) {   // what is dropped is cleared in the packed result
+            const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
+            philox<2>(stream, group, w);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) parts(mul2(two(v[j], v[j + 1]), two(p.drop.scale)), v[j], v[j + 1]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]) & kept_halves(w[j], p.drop);
+            put_words(h, w);
+            return;
+          } else if constexpr (DROP) {
             const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
             philox<2>(stream, group, w);
 #pragma unroll
@@ -313,19 +320,28 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           put(h, out);
         };
-        // a step's accumulator is read while the one before is worked on
         auto pass = [&](auto is_z, const CUtensorMap& map) {
-          uint32_t a0[16], a1[16];
-          ptx::tmem_ld_32x16(acc, a0);
-          ptx::tmem_ld_wait();
+          uint32_t a0[16];
+          if constexpr (DROP && RES) {   // (the registers are needed otherwise)
 #pragma unroll 1
-          for (int h = 0; h < 4 && cols > 0; h += 2) {
-            ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
-            step(is_z, h, a0);
+            for (int h = 0; h < 4; ++h) {
+              ptx::tmem_ld_32x16(acc + h * 16, a0);
+              ptx::tmem_ld_wait();
+              step(is_z, h, a0);
+            }
+          } else {   // a step's accumulator is read while the one before is worked on
+            uint32_t a1[16];
+            ptx::tmem_ld_32x16(acc, a0);
             ptx::tmem_ld_wait();
-            if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
-            step(is_z, h + 1, a1);
-            ptx::tmem_ld_wait();
+#pragma unroll 1
+            for (int h = 0; h < 4; h += 2) {
+              ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
+              step(is_z, h, a0);
+              ptx::tmem_ld_wait();
+              if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
+              step(is_z, h + 1, a1);
+              ptx::tmem_ld_wait();
+            }
           }
           ptx::fence_proxy_async_smem();
           __syncwarp();

@@ -24,6 +24,7 @@ struct Drop {
   const uint64_t *seed_dev, *offset_dev;
   uint64_t* used;
   uint32_t above;   // an element stays where its number, as the high half of a word, is above this
+  uint32_t low15, low_half;   // the same for both halves of a word at once, see kept_halves
   float scale;
   int32_t on;
 };
@@ -90,6 +91,16 @@ __device__ __forceinline__ void add_kept2(float& lo, float& hi, float v0, float 
   add_kept(hi, v1, w, d);
 }
 
+// All ones in the halves of w that hold 16-bit numbers u >= t, in four instructions.  With the top bits apart, (u | 2^15) -
+// (t mod 2^15) keeps its top bit exactly where u mod 2^15 >= t mod 2^15 and never borrows from the other half; u >= t is
+// then "that bit or u's" for t below 2^15, "and" from there on: the majority with low_half.
+__device__ __forceinline__ uint32_t kept_halves(uint32_t w, const Drop& d) {
+  const uint32_t r = (w | 0x80008000u) - d.low15;
+  const uint32_t top = (w & r) | (d.low_half & (w | r));
+  uint32_t m;
+  asm("prmt.b32 %0, %1, 0, 0xbb99;" : "=r"(m) : "r"(top));   // the sign bits of bytes 1 and 3, all over their halves
+  return m;
+}
 // out += drop(v) of four elements from number n (a multiple of 4) on.
 __device__ __forceinline__ void add_dropped(float (&out)[4], const float (&v)[4], uint64_t n, const Stream& s, const Drop& d) {
   if (d.on) {
@@ -157,6 +168,14 @@ __device__ __forceinline__ F2 add2(F2 a, F2 b) {
   return r;
 }
 
+// the sign of x, and |x| up to a bound; NaN stays
+__device__ __forceinline__ float clamp_abs(float x, float most) {
+  float y;
+  asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(most));
+  return y;
+}
+
+constexpr float kInvSqrt2Pi = 0.3989422804014327f;
 constexpr float kLog2e = 1.4426950408889634f;
 // 2 sqrt(2/pi) and 0.044715 times that: gelu_tanh(z) = z / (1 + exp(-(A z + B z^3)))
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.071354816272600247f;
@@ -166,16 +185,6 @@ constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.071354816272600247f;
 //   exp(a^2/2) a Phi(-a) = S(t), c = 0.4, off by at most 8.6e-5 (S + 0.002).  With it gelu(z) =
 //       max(z, 0) - |z| Phi(-|z|) needs no case for infinities: t, exp(-a^2/2) and S stay finite.
 //   exp(a^2/2) Phi(-a) = Q(t), c = 0.38, off by at most 3.7e-5 Q.
-__device__ __forceinline__ float tail_poly(float a) {
-  const float t = rcp(fmaf(0.38f, a, 1.f));
-  float q = -0.0906074270606041f;
-  q = fmaf(q, t, 0.1908050775527954f);
-  q = fmaf(q, t, 0.08993600308895111f);
-  q = fmaf(q, t, 0.15882457792758942f);
-  q = fmaf(q, t, 0.15100638568401337f);
-  return fmaf(q, t, 1.705829163256567e-05f);
-}
-
 // For fp32 data.
 template <int ACT>
 __device__ __forceinline__ float act(float z) {
@@ -250,38 +259,67 @@ __device__ __forceinline__ float act_of(int a, float z) {
   return z;
 }
 
-// FAST: for results that are rounded to bf16.
-template <int ACT, bool FAST>
+// act' for fp32 data.
+template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
-  constexpr float kInvSqrt2Pi = 0.3989422804014327f;
   if constexpr (ACT == LBP_ACT_NONE) {
     return 1.f;
   } else if constexpr (ACT == LBP_ACT_RELU) {
     return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;   // (NaN stays)
   } else if constexpr (ACT == LBP_ACT_GELU) {
-    if constexpr (FAST) {
-      // Phi(z) + z phi(z) = 1/2 + sign(z) (1/2 - g), g = exp(-a^2/2) (Q - a / sqrt(2 pi)) <= 1/2, a = |z|
-      const float a = at_most(fabsf(z), 100.f);
-      const float e = ex2(a * (a * (-0.5f * kLog2e)));
-      const float d = fmaf(-e, fmaf(-kInvSqrt2Pi, a, tail_poly(a)), 0.5f);
-      return 0.5f + copysignf(d, z);
-    } else {
-      const float c = at_most(at_least(z, -100.f), 100.f);
-      return fmaf(c * kInvSqrt2Pi, expf(-0.5f * c * c), 0.5f * erfcf(c * -0.70710678118654752f));
-    }
+    const float c = clamp_abs(z, 100.f);
+    return fmaf(c * kInvSqrt2Pi, expf(-0.5f * c * c), 0.5f * erfcf(c * -0.70710678118654752f));
   } else if constexpr (ACT == LBP_ACT_GELU_TANH) {
     // s (1 + z (1 - s) u') with s = 1 / (1 + exp(-u))
-    const float c = at_most(at_least(z, -12.f), 12.f);   // (s is 0 and 1 there)
+    const float c = clamp_abs(z, 12.f);   // (s is 0 and 1 there)
     const float c2 = c * c;
     const float u = c * fmaf(kTanhB, c2, kTanhA), du = fmaf(3.f * kTanhB, c2, kTanhA);
-    const float e = FAST ? ex2(-kLog2e * u) : expf(-u);
-    const float s = FAST ? rcp(1.f + e) : 1.f / (1.f + e);
+    const float s = 1.f / (1.f + expf(-u));
     return fmaf(c * du, s * (1.f - s), s);
   } else {
-    const float c = at_most(at_least(z, -100.f), 100.f);   // (s is 0 and 1 there)
-    const float e = FAST ? ex2(-kLog2e * c) : expf(-c);
-    const float s = FAST ? rcp(1.f + e) : 1.f / (1.f + e);
+    const float c = clamp_abs(z, 100.f);   // (s is 0 and 1 there)
+    const float s = 1.f / (1.f + expf(-c));
     return fmaf(c, s * (1.f - s), s);
+  }
+}
+
+// g act'(z) for results that are rounded to bf16: of two numbers.
+template <int ACT>
+__device__ __forceinline__ void times_slope_fast(float& g0, float& g1, float z0, float z1) {
+  if constexpr (ACT == LBP_ACT_RELU) {
+    g0 = z0 > 0.f ? g0 : z0 <= 0.f ? 0.f : z0;   // (NaN stays)
+    g1 = z1 > 0.f ? g1 : z1 <= 0.f ? 0.f : z1;
+  } else if constexpr (ACT == LBP_ACT_GELU) {
+    // Phi(z) + z phi(z) = 1/2 + sign(z) d, d = 1/2 - exp(-a^2/2) (Q - a / sqrt(2 pi)) >= 0, a = |z|
+    const F2 a = two(at_most(fabsf(z0), 100.f), at_most(fabsf(z1), 100.f));
+    float x, y, e0, e1;
+    parts(fma2(a, two(0.38f), two(1.f)), x, y);
+    const F2 t = two(rcp(x), rcp(y));
+    parts(mul2(a, mul2(a, two(-0.5f * kLog2e))), e0, e1);
+    F2 q = fma2(t, two(0.0906074270606041f), two(-0.1908050775527954f));   // -Q
+    q = fma2(q, t, two(-0.08993600308895111f));
+    q = fma2(q, t, two(-0.15882457792758942f));
+    q = fma2(q, t, two(-0.15100638568401337f));
+    q = fma2(q, t, two(-1.705829163256567e-05f));
+    parts(fma2(two(ex2(e0), ex2(e1)), fma2(a, two(kInvSqrt2Pi), q), two(0.5f)), x, y);
+    parts(mul2(two(g0, g1), add2(two(copysignf(x, z0), copysignf(y, z1)), two(0.5f))), g0, g1);
+  } else if constexpr (ACT == LBP_ACT_GELU_TANH || ACT == LBP_ACT_SILU) {
+    constexpr float kMost = ACT == LBP_ACT_SILU ? 100.f : 12.f;   // (s is 0 and 1 there)
+    const F2 c = two(clamp_abs(z0, kMost), clamp_abs(z1, kMost));
+    F2 u, v = c;   // the exponent; z u'
+    if constexpr (ACT == LBP_ACT_SILU) {
+      u = mul2(c, two(-kLog2e));
+    } else {
+      const F2 c2 = mul2(c, c);
+      u = mul2(c, fma2(c2, two(-kLog2e * kTanhB), two(-kLog2e * kTanhA)));
+      v = mul2(c, fma2(c2, two(3.f * kTanhB), two(kTanhA)));
+    }
+    float x, y;
+    parts(u, x, y);
+    parts(add2(two(ex2(x), ex2(y)), two(1.f)), x, y);
+    const F2 s = two(rcp(x), rcp(y));
+    // s + v s (1 - s)
+    parts(mul2(two(g0, g1), fma2(mul2(v, s), fma2(s, two(-1.f), two(1.f)), s)), g0, g1);
   }
 }
 
@@ -324,6 +362,67 @@ int with_act(int a, F f) {
     case LBP_ACT_SILU: return f(std::integral_constant<int, LBP_ACT_SILU>{});
   }
   return LBP_ERR_SHAPE;
+}
+
+// drop(g) act'(z) of a vector each of g and z, in fp32: u vectors at once.
+template <class T, int ACT, bool DROP, int U>
+__device__ __forceinline__ void gradient(const uint4 (&g)[U], const uint4 (&z)[U], const uint64_t (&number)[U], const Stream& s,
+                                         const Drop& d, float (&out)[U][Vec<T>::N]) {
+  using V = Vec<T>;
+  uint32_t w[DROP ? 4 * U : 1];
+  if constexpr (DROP) {
+    uint64_t group[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) group[u] = number[u] >> 3;
+    philox<U>(s, group, w);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float v[V::N];
+    if constexpr (DROP && V::N == 8) {
+      // what is dropped leaves as zero, g and z, before any arithmetic
+      const uint32_t m[4] = {kept_halves(w[4 * u], d), kept_halves(w[4 * u + 1], d), kept_halves(w[4 * u + 2], d),
+                             kept_halves(w[4 * u + 3], d)};
+      V::unpack(make_uint4(g[u].x & m[0], g[u].y & m[1], g[u].z & m[2], g[u].w & m[3]), v);
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) parts(mul2(two(v[j], v[j + 1]), two(d.scale)), v[j], v[j + 1]);
+      if constexpr (ACT != LBP_ACT_NONE) {
+        float x[8];
+        V::unpack(make_uint4(z[u].x & m[0], z[u].y & m[1], z[u].z & m[2], z[u].w & m[3]), x);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) times_slope_fast<ACT>(v[j], v[j + 1], x[j], x[j + 1]);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) out[u][j] = v[j];
+      continue;
+    }
+    V::unpack(g[u], v);
+    if constexpr (ACT != LBP_ACT_NONE) {
+      float x[V::N];
+      V::unpack(z[u], x);
+#pragma unroll
+      for (int j = 0; j < V::N; j += 2) {
+        if constexpr (V::kFast) {
+          times_slope_fast<ACT>(v[j], v[j + 1], x[j], x[j + 1]);
+        } else {
+          v[j] *= act_slope<ACT>(x[j]);
+          v[j + 1] *= act_slope<ACT>(x[j + 1]);
+        }
+      }
+    }
+    if constexpr (DROP) {
+      const bool upper = V::N == 4 && (number[u] & 4u) != 0;
+#pragma unroll
+      for (int j = 0; j < V::N; j += 2) {
+        out[u][j] = out[u][j + 1] = 0.f;
+        const uint32_t word = V::N == 8 ? w[4 * u + j / 2] : upper ? w[4 * u + 2 + j / 2] : w[4 * u + j / 2];
+        add_kept2(out[u][j], out[u][j + 1], v[j], v[j + 1], word, d);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V::N; ++j) out[u][j] = v[j];
+    }
+  }
 }
 
 // ---- launchers -----------------------------------------------------------------------------
