@@ -151,6 +151,10 @@ static int run_grid(const void* g_y, const void* z, void* g_z, int B, int H, int
   return launch_pointwise(c, st);
 }
 
+static GradOf grad_of(const void* z, int H, int W, int C, const lbp_epilogue& e) {
+  return GradOf{e.act != LBP_ACT_NONE ? z : nullptr, e.act, e.first, resolve_view(&e.number, H, W, C), drop_of(e)};
+}
+
 static size_t grid_bytes(long long tokens, int C, int dtype) {
   return align_up(static_cast<size_t>(tokens) * C * elem_size(dtype), 1024);
 }
@@ -162,8 +166,17 @@ static lbp_extras with_dense_gradient(const lbp_extras* ex) {
   d.gy_extra_pitch = 0;
   return d;
 }
+// Whether the projection of lbp_backward_act may form the gradient of the grid's tokens itself.  (The sum for a bias
+// then has to come from the coefficients: only with the basis (0, 0) among them.)
+static bool may_form(const lbp_layer& L, int r, bool x_hat) {
+  return project_forms_gradient(L.dtype, L.B, L.H, L.W, L.k, r) && (x_hat || r < L.k * L.k);
+}
+// Workspace of the call on g_z, dense or with g_y's strides.
 static size_t inner_bytes(const lbp_layer* layer, int r, const lbp_extras* ex, bool x_hat) {
-  return (x_hat ? lbp_workspace_bytes_projected : lbp_workspace_bytes_ex)(layer, r, ex);
+  const auto of = x_hat ? lbp_workspace_bytes_projected : lbp_workspace_bytes_ex;
+  const lbp_extras d = with_dense_gradient(ex);
+  const size_t as_given = of(layer, r, ex), dense = of(layer, r, &d);
+  return as_given == 0 || dense == 0 ? 0 : align_up(as_given > dense ? as_given : dense, 1024);
 }
 
 }  // namespace layer
@@ -257,7 +270,9 @@ int lbp_dropout(const void* x, const void* residual, void* y, long long rows, in
 
 size_t lbp_project_grad_workspace_bytes(int B, int H, int W, int C, int k, int r, int dtype) {
   if (check_shape(B, H, W, C, k, dtype) != LBP_OK || r < 1 || r > k * k) return 0;
-  return 1024 + grid_bytes(static_cast<long long>(B) * H * W, C, dtype);
+  // where the projection does not form it, the gradient lies behind the status block
+  return project_forms_gradient(dtype, B, H, W, k, r) ? kStatusBytes
+                                                      : 1024 + grid_bytes(static_cast<long long>(B) * H * W, C, dtype);
 }
 
 int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, int W, int C, int k,
@@ -275,6 +290,14 @@ int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, 
   if (ws == nullptr || ws_bytes < lbp_project_grad_workspace_bytes(B, H, W, C, k, r, dtype)) return LBP_ERR_WORKSPACE;
   if (int s = check_device_arch()) return s;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const GradOf of = grad_of(z, H, W, C, e);
+  const bool as_it_is = e.act == LBP_ACT_NONE && !of.drop.on && e.used == nullptr;   // g_z is g_y
+  if (as_it_is || project_forms_gradient(dtype, B, H, W, k, r)) {
+    if (!as_it_is) set_projection_gradient(&of);
+    const int s = launch_project(g_y, t_hat, dtype, B, H, W, C, plan, static_cast<uint32_t*>(ws), st, 0.f, view);
+    set_projection_gradient(nullptr);
+    return s;
+  }
   void* const g_z = static_cast<uint8_t*>(ws) + 1024;
   if (int s = run_grid(g_y, z, g_z, B, H, W, C, dtype, view, e, st)) return s;
   return launch_project(g_z, t_hat, dtype, B, H, W, C, plan, static_cast<uint32_t*>(ws), st);
@@ -282,10 +305,12 @@ int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, 
 
 size_t lbp_workspace_bytes_act(const lbp_layer* layer, int r, const lbp_extras* ex, int x_hat) {
   const lbp_extras d = with_dense_gradient(ex);
-  const size_t inner = inner_bytes(layer, r, &d, x_hat != 0);
+  const size_t inner = inner_bytes(layer, r, ex, x_hat != 0);
   if (inner == 0) return 0;
-  return align_up(inner, 1024) + grid_bytes(static_cast<long long>(layer->B) * layer->H * layer->W, layer->Cout, layer->dtype) +
-         grid_bytes(d.n_extra, layer->Cout, layer->dtype);
+  return inner + grid_bytes(d.n_extra, layer->Cout, layer->dtype) +
+         (may_form(*layer, r, x_hat != 0) && d.g_bias == nullptr
+              ? 0
+              : grid_bytes(static_cast<long long>(layer->B) * layer->H * layer->W, layer->Cout, layer->dtype));
 }
 
 int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const void* W, void* g_x, void* g_W,
@@ -302,6 +327,8 @@ int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const vo
       grad->number_extra >= (int64_t{1} << 50))
     return LBP_ERR_SHAPE;
   if (!in_quads(grad->first_extra, dtype) || !in_quads(grad->number_extra, dtype)) return LBP_ERR_ALIGN;
+  if (n_extra > 0)
+    if (int s = check_pitch(ex->gy_extra_pitch, C, dtype)) return s;
   // the call as it is, for what is wrong with it apart from the epilogue
   if (int s = backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, true)) return s;
   const size_t need = lbp_workspace_bytes_act(layer, r, ex, x_hat != nullptr);
@@ -309,21 +336,31 @@ int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const vo
   if (int s = check_device_arch()) return s;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   lbp_extras d = with_dense_gradient(ex);
-  const size_t inner = align_up(inner_bytes(layer, r, &d, x_hat != nullptr), 1024);
-  uint8_t* const g_z = static_cast<uint8_t*>(ws) + inner;
-  if (int s = run_grid(g_y, grad->z, g_z, layer->B, layer->H, layer->W, C, dtype, ex != nullptr ? &ex->gy_view : nullptr, e, st))
-    return s;
+  const size_t inner = inner_bytes(layer, r, ex, x_hat != nullptr);
+  uint8_t* const g_ze = static_cast<uint8_t*>(ws) + inner;
   if (n_extra > 0) {
     lbp_epilogue ee = e;
     ee.first = grad->first_extra;
     ee.number = lbp_view{0, 0, grad->number_extra};
     ee.used = nullptr;
-    uint8_t* const g_ze = g_z + grid_bytes(static_cast<long long>(layer->B) * layer->H * layer->W, C, dtype);
     if (int s = run_rows(ex->gy_extra, grad->z_extra, nullptr, g_ze, n_extra, C, dtype, ex->gy_extra_pitch,
                          ex->gy_extra_pitch, 0, 0, ee, st))
       return s;
     d.gy_extra = g_ze;
   }
+  bool dc = false;
+  for (int q = 0; q < r; ++q) dc |= set[q].i == 0 && set[q].j == 0;
+  if (may_form(*layer, r, x_hat != nullptr) && (dc || d.g_bias == nullptr)) {
+    d.gy_view = ex != nullptr ? ex->gy_view : lbp_view{0, 0, 0};
+    const GradOf of = grad_of(grad->z, layer->H, layer->W, C, e);
+    set_projection_gradient(&of);
+    const int s = backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, &d, ws, inner, stream, false);
+    set_projection_gradient(nullptr);
+    return s;
+  }
+  uint8_t* const g_z = g_ze + grid_bytes(n_extra, C, dtype);
+  if (int s = run_grid(g_y, grad->z, g_z, layer->B, layer->H, layer->W, C, dtype, ex != nullptr ? &ex->gy_view : nullptr, e, st))
+    return s;
   return backward_ex_call(x, x_hat, g_z, W, g_x, g_W, layer, set, r, &d, ws, inner, stream, false);
 }
 

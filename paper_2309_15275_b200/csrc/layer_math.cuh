@@ -364,6 +364,25 @@ int with_act(int a, F f) {
   return LBP_ERR_SHAPE;
 }
 
+// drop(g) act'(z) of eight bf16 numbers each, where m has all ones in the halves that stay: what is dropped leaves as
+// zero, g and z, before any arithmetic.
+template <int ACT, bool DROP>
+__device__ __forceinline__ void masked_gradient(uint4 g, uint4 z, const uint32_t* m, const Drop& d, float (&v)[8]) {
+  using V = Vec<__nv_bfloat16>;
+  if constexpr (DROP) g = make_uint4(g.x & m[0], g.y & m[1], g.z & m[2], g.w & m[3]);
+  V::unpack(g, v);
+  if constexpr (DROP) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) parts(mul2(two(v[j], v[j + 1]), two(d.scale)), v[j], v[j + 1]);
+  }
+  if constexpr (ACT != LBP_ACT_NONE) {
+    float x[8];
+    if constexpr (DROP) z = make_uint4(z.x & m[0], z.y & m[1], z.z & m[2], z.w & m[3]);
+    V::unpack(z, x);
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) times_slope_fast<ACT>(v[j], v[j + 1], x[j], x[j + 1]);
+  }
+}
 // drop(g) act'(z) of a vector each of g and z, in fp32: u vectors at once.
 template <class T, int ACT, bool DROP, int U>
 __device__ __forceinline__ void gradient(const uint4 (&g)[U], const uint4 (&z)[U], const uint64_t (&number)[U], const Stream& s,
@@ -379,19 +398,13 @@ __device__ __forceinline__ void gradient(const uint4 (&g)[U], const uint4 (&z)[U
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float v[V::N];
-    if constexpr (DROP && V::N == 8) {
-      // what is dropped leaves as zero, g and z, before any arithmetic
-      const uint32_t m[4] = {kept_halves(w[4 * u], d), kept_halves(w[4 * u + 1], d), kept_halves(w[4 * u + 2], d),
-                             kept_halves(w[4 * u + 3], d)};
-      V::unpack(make_uint4(g[u].x & m[0], g[u].y & m[1], g[u].z & m[2], g[u].w & m[3]), v);
+    if constexpr (V::N == 8) {
+      uint32_t m[4] = {};
+      if constexpr (DROP) {
 #pragma unroll
-      for (int j = 0; j < 8; j += 2) parts(mul2(two(v[j], v[j + 1]), two(d.scale)), v[j], v[j + 1]);
-      if constexpr (ACT != LBP_ACT_NONE) {
-        float x[8];
-        V::unpack(make_uint4(z[u].x & m[0], z[u].y & m[1], z[u].z & m[2], z[u].w & m[3]), x);
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) times_slope_fast<ACT>(v[j], v[j + 1], x[j], x[j + 1]);
+        for (int j = 0; j < 4; ++j) m[j] = kept_halves(w[4 * u + j], d);
       }
+      masked_gradient<ACT, DROP>(g[u], z[u], m, d, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) out[u][j] = v[j];
       continue;
@@ -458,6 +471,20 @@ struct PointCall {
   Drop drop;
 };
 int launch_pointwise(const PointCall& c, cudaStream_t stream);
+
+// What lbp_project's tensor is formed from where it is a gradient.
+struct GradOf {
+  const void* z;      // laid out as g_y, or null without an activation
+  int32_t act;
+  int64_t first;
+  lbp_view number;    // resolved
+  Drop drop;
+};
+// Whether the projection kernel of such a call forms the gradient itself.
+bool project_forms_gradient(int dtype, int B, int H, int W, int k, int r);
+// While set (per calling thread), the first tensor of a projection is what it is formed from.
+void set_projection_gradient(const GradOf* of);
+const GradOf* projection_gradient();
 
 }  // namespace layer
 }  // namespace lbp

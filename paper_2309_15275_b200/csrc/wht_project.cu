@@ -240,6 +240,19 @@ static int launch_t(const CUtensorMap* tmaps, T* out0, T* out1, const ProjParams
   return LBP_ERR_BLOCK;
 }
 
+// (the tcgen05 form addresses coefficient rows with 32 bits)
+static bool runs_on_umma(int dtype, long long nb, int k, int r) {
+  return dtype == LBP_BF16 && tune_options().umma && project_umma_supported(k, r) && nb * r < (1ll << 31);
+}
+static thread_local const layer::GradOf* g_gradient = nullptr;
+namespace layer {
+void set_projection_gradient(const GradOf* of) { g_gradient = of; }
+const GradOf* projection_gradient() { return g_gradient; }
+bool project_forms_gradient(int dtype, int B, int H, int W, int k, int r) {
+  return runs_on_umma(dtype, static_cast<long long>(B) * blocks_along(H, k) * blocks_along(W, k), k, r);
+}
+}  // namespace layer
+
 int launch_project2(const void* t0, void* out0, int C0, const void* t1, void* out1, int C1,
                     int dtype, int B, int H, int W, const BasisPlan& bp,
                     uint32_t* status, cudaStream_t stream, float scale0, float scale1,
@@ -270,11 +283,11 @@ int launch_project2(const void* t0, void* out0, int C0, const void* t1, void* ou
   LBP_CUDA_TRY(cudaGetDevice(&dev));
   LBP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
 
-  // (the tcgen05 form addresses coefficient rows with 32 bits)
-  const bool rows_fit = static_cast<long long>(p.nb) * bp.r < (1ll << 31);
-  if (dtype == LBP_BF16 && tune_options().umma && project_umma_supported(K, bp.r) && rows_fit)
+  const layer::GradOf* const of = layer::projection_gradient();
+  if (runs_on_umma(dtype, p.nb, K, bp.r))
     return launch_project_umma(t0, out0, C0, view0, t1, out1, C1, view1, B, H, W, bp, p.scale[0], p.scale[1],
-                               sms, status, stream);
+                               sms, status, stream, of);
+  if (of != nullptr) return LBP_ERR_DTYPE;   // (the caller has asked project_forms_gradient)
   CUtensorMap tmaps[2];
   if (int e = encode_block_tensor_map(&tmaps[0], t0, dtype, B, H, W, C0, K, box_c, false, view0)) return e;
   if (t1 != nullptr) {

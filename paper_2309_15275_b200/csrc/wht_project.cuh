@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include "layer_math.cuh"
 #include "lbp_internal.h"
 
 namespace lbp {
@@ -30,11 +31,11 @@ struct ProjCfg {
 };
 
 // tcgen05 tensor cores (bf16): orders 8 and 16 at r <= 48, order 4 at every rank.
-// Coefficients are written densely (block blk: rows blk * r ..); t1 may be null.
+// Coefficients are written densely (block blk: rows blk * r ..); t1 may be null.  of: what t0 is formed into first.
 bool project_umma_supported(int k, int r);
 int launch_project_umma(const void* t0, void* out0, int C0, const lbp_view* view0, const void* t1,
                         void* out1, int C1, const lbp_view* view1, int B, int H, int W,
                         const BasisPlan& bp, float scale0, float scale1, int sms, uint32_t* status,
-                        cudaStream_t stream);
+                        cudaStream_t stream, const layer::GradOf* of);
 
 }  // namespace lbp

@@ -34,8 +34,14 @@
 // epilogue is a chain of about a microsecond: two groups held an SM to 62 GB/s).
 // Every wait is bounded; a timeout raises the status word and all roles fall through to
 // the exit.
+//
+// GRAD: tensor 0 is g_z = drop(g_y) act'(z), which is never in memory.  A stage holds the boxes of g_y and z; sixteen
+// more warps, in two sets that take turns, overwrite g_y with g_z where it lies (both have the same swizzle, so a thread's 16 bytes of
+// the one lie like those of the other) before the tensor core reads it.  One epilogue group is enough: what bounds it is
+// the arithmetic of those warps.
 #include <cuda_bf16.h>
 
+#include "layer_math.cuh"
 #include "lbp_internal.h"
 #include "ptx_sm100.cuh"
 #include "wht_device.cuh"
@@ -49,7 +55,9 @@ constexpr int kTileBytes = 64 * 128;             // 64 tokens x 64 channels of b
 constexpr int kStageBytes = 4 * kTileBytes;      // 32 KB: an item, or a quarter of one at order 16
 constexpr int kProducers = 4;
 constexpr int kMaxGroups = 4;                    // epilogue warpgroups
-constexpr int kThreads = (8 + 4 * kMaxGroups) * 32;
+constexpr int kGradWarps = 16;                   // (GRAD, with one epilogue group)
+template <bool GRAD>
+constexpr int kThreadsOf = (8 + (GRAD ? 4 + kGradWarps : 4 * kMaxGroups)) * 32;
 constexpr int kMaxStages = 6;
 constexpr int kBarBytes = 256;
 constexpr int kSmemMax = 227 * 1024;
@@ -73,6 +81,16 @@ struct Params {
   int32_t stages, groups;        // ring stages; epilogue warpgroups at work
   Steps step[2];
 };
+
+// GRAD: what tensor 0 is formed from.
+struct Grad {
+  CUtensorMap z;
+  int32_t act;                // none: no z
+  int64_t first;              // numbers of elements
+  lbp_view number;
+  layer::Drop drop;
+};
+struct NoGrad {};
 
 // Chunk number -> tensor, block and column.  The position is decoded once, then
 // moved by precomputed steps with carries.
@@ -140,6 +158,49 @@ __device__ __forceinline__ bool group_or(int id, bool pred) {
   return any != 0;
 }
 
+// 512 pieces of 16 bytes of a chunk, by 64 threads: g_y, at `at`, becomes g_z.  The thread's piece i has the number
+// number + (i & 1) step0 + (i >> 1) step1.
+template <int ACT, bool DROP>
+__device__ __forceinline__ void form_gradient(uint8_t* at, uint64_t number, int64_t step0, int64_t step1, const layer::Stream& s,
+                                              const layer::Drop& d) {
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h, at += 4096, number += static_cast<uint64_t>(2 * step1)) {
+    uint32_t m[16] = {};
+    if constexpr (DROP) {   // the choices of four pieces first: eight independent chains of multiplications
+      const uint64_t group[4] = {number >> 3, (number + static_cast<uint64_t>(step0)) >> 3,
+                                 (number + static_cast<uint64_t>(step1)) >> 3, (number + static_cast<uint64_t>(step0 + step1)) >> 3};
+      layer::philox<4>(s, group, m);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) m[j] = layer::kept_halves(m[j], d);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 g = *reinterpret_cast<const uint4*>(at + i * 1024);
+      uint4 z = make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (ACT != LBP_ACT_NONE) z = *reinterpret_cast<const uint4*>(at + kStageBytes + i * 1024);
+      float v[8];
+      layer::masked_gradient<ACT, DROP>(g, z, m + 4 * i, d, v);
+      *reinterpret_cast<uint4*>(at + i * 1024) = layer::Vec<__nv_bfloat16>::pack(v);
+    }
+  }
+}
+__device__ __forceinline__ void form_gradient(int act, uint8_t* at, uint64_t number, int64_t step0, int64_t step1,
+                                              const layer::Stream& s, const layer::Drop& d) {
+  auto with = [&](auto a) {
+    if (d.on)
+      form_gradient<decltype(a)::value, true>(at, number, step0, step1, s, d);
+    else
+      form_gradient<decltype(a)::value, false>(at, number, step0, step1, s, d);
+  };
+  switch (act) {
+    case LBP_ACT_NONE: return with(std::integral_constant<int, LBP_ACT_NONE>{});
+    case LBP_ACT_RELU: return with(std::integral_constant<int, LBP_ACT_RELU>{});
+    case LBP_ACT_GELU: return with(std::integral_constant<int, LBP_ACT_GELU>{});
+    case LBP_ACT_GELU_TANH: return with(std::integral_constant<int, LBP_ACT_GELU_TANH>{});
+    default: return with(std::integral_constant<int, LBP_ACT_SILU>{});
+  }
+}
+
 // Output maps of the tensors: boxes of the rows of a whole "block" (order 4: of the
 // four blocks of a strip) and, order 4, of the last strip of a row of blocks.
 struct OutMaps {
@@ -147,12 +208,14 @@ struct OutMaps {
 };
 
 // K: order; NB: N / 16 (order 4: what the epilogue reads of a block's 16 columns, / 4)
-template <int K, int NB>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int K, int NB, class G>
+__global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
     wht_project_umma_kernel(const __grid_constant__ CUtensorMap tmap0,
                             const __grid_constant__ CUtensorMap tmap1,
                             const __grid_constant__ OutMaps om, const __grid_constant__ Params p,
-                            const __grid_constant__ MmaPlan mp) {
+                            const __grid_constant__ MmaPlan mp, const __grid_constant__ G grad) {
+  constexpr bool GRAD = std::is_same<G, Grad>::value;
+  constexpr int kThreads = kThreadsOf<GRAD>;
   constexpr int kParts = K == 16 ? 4 : 1;
   constexpr int kN = K == 4 ? 16 : NB * 16;   // columns of one MMA
   constexpr int kPanelBytes = kN * 128;       // 64 tokens x N rows
@@ -160,7 +223,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint8_t* sB = smem + p.stages * kStageBytes;
+  bool with_z = false;
+  if constexpr (GRAD) with_z = grad.act != LBP_ACT_NONE;
+  const int stage_bytes = with_z ? 2 * kStageBytes : kStageBytes;
+  uint8_t* sB = smem + p.stages * stage_bytes;
   uint8_t* sOut = sB + kParts * kPanelBytes;
   const int rows = p.r * p.per_strip;             // coefficient rows of a chunk
   const int out_bytes = rows * 128;
@@ -168,7 +234,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* empty_bar = full_bar + kMaxStages;
   uint64_t* acc_full = empty_bar + kMaxStages;   // [kSlots]
   uint64_t* acc_empty = acc_full + kSlots;       // [kSlots]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + kSlots);
+  uint64_t* ready_bar = acc_empty + kSlots;      // [kMaxStages], GRAD: g_z is in place
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ready_bar + (GRAD ? kMaxStages : 0));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -181,6 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int s = 0; s < p.stages; ++s) {
       ptx::mbar_init(&full_bar[s], kProducers);
       ptx::mbar_init(&empty_bar[s], 1);
+      if constexpr (GRAD) ptx::mbar_init(&ready_bar[s], kGradWarps);
     }
     for (int s = 0; s < kSlots; ++s) {
       ptx::mbar_init(&acc_full[s], 1);
@@ -264,15 +332,21 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (have) {
             // the whole box counts, also where it hangs over the tensor (zero fill)
-            ptx::mbar_expect_tx(&full_bar[s], kTileBytes);
+            const bool z_too = with_z && c.which == 0;
+            ptx::mbar_expect_tx(&full_bar[s], z_too ? 2 * kTileBytes : kTileBytes);
             constexpr int kBoxes = K == 4 ? 4 : 1;
+            auto fetch = [&](const CUtensorMap* map, uint8_t* to) {
 #pragma unroll
-            for (int j = 0; j < kBoxes; ++j)
-              ptx::tma_load_4d_hint(smem + s * kStageBytes + warp * kTileBytes + j * (kTileBytes / kBoxes),
-                                    c.which ? &tmap1 : &tmap0, &full_bar[s], ch,
-                                    static_cast<int32_t>(c.bw * kBoxW) + j * 4,
-                                    static_cast<int32_t>(c.bh * (K == 16 ? 16 : kBoxH) + part * 4),
-                                    static_cast<int32_t>(c.b), stream_once);
+              for (int j = 0; j < kBoxes; ++j)
+                ptx::tma_load_4d_hint(to + warp * kTileBytes + j * (kTileBytes / kBoxes), map, &full_bar[s], ch,
+                                      static_cast<int32_t>(c.bw * kBoxW) + j * 4,
+                                      static_cast<int32_t>(c.bh * (K == 16 ? 16 : kBoxH) + part * 4),
+                                      static_cast<int32_t>(c.b), stream_once);
+            };
+            fetch(c.which ? &tmap1 : &tmap0, smem + s * stage_bytes);
+            if constexpr (GRAD) {
+              if (z_too) fetch(&grad.z, smem + s * stage_bytes + kStageBytes);
+            }
           } else {
             ptx::mbar_arrive(&full_bar[s]);   // no such chunk: what lies in the stage is multiplied and dropped
           }
@@ -301,12 +375,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         for (int part = 0; part < kParts; ++part) {
-          if (!ptx::mbar_wait(&full_bar[s], phase, p.status, (6u << 16) | 3u)) {
+          if (!ptx::mbar_wait(GRAD ? &ready_bar[s] : &full_bar[s], phase, p.status, (6u << 16) | 3u)) {
             ok = false;
             break;
           }
           ptx::tc_fence_after_sync();
-          const uint32_t sa = ptx::smem_u32(smem + s * kStageBytes);
+          const uint32_t sa = ptx::smem_u32(smem + s * stage_bytes);
           for (int h = 0; h < (second ? 2 : 1); ++h) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
@@ -330,6 +404,49 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::mma_commit(&acc_full[slot]);
       }
       if (!ok) *abort_flag = 1;
+    }
+  } else if (GRAD && warp >= 12) {
+    // =========================== g_z ===========================
+    if constexpr (GRAD) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      const layer::Stream stream = grad.drop.on ? layer::open_stream(grad.drop) : layer::Stream{};
+      if (blockIdx.x == 0 && threadIdx.x == 12 * 32) layer::note_used(grad.drop);
+      // two sets of eight warps take turns on the stages, in a set two warps to a chunk
+      const int set = (warp - 12) >> 3, mine = ((warp - 12) & 7) >> 1, tid = threadIdx.x & 63;
+      const int row = tid >> 3, piece = (tid & 7) ^ row;   // token row of the box (and 8 i on); channels 8 piece on
+      const int u0 = K == 4 ? row >> 2 : 0, v0 = K == 4 ? row & 3 : row;
+      const int64_t step0 = K == 8 ? grad.number.row : K == 16 ? 8 * grad.number.token : 2 * grad.number.row;
+      const int64_t step1 = K == 8 ? 2 * grad.number.row : K == 16 ? grad.number.row : 4 * grad.number.token;
+      Cursor c;
+      c.decode(p, 4 * blockIdx.x + mine);
+      bool ok = true;
+      int s = 0, turn = 0;
+      uint32_t phase = 0;
+      for (uint32_t n = 0; n < my_items && ok; ++n) {
+        const bool form = c.chunk < p.n_chunks && c.which == 0;
+        const uint64_t n0 = static_cast<uint64_t>(
+            grad.first + c.b * grad.number.image + (c.bh * (K == 16 ? 16 : kBoxH) + u0) * grad.number.row +
+            (static_cast<int64_t>(c.bw) * kBoxW + v0) * grad.number.token + static_cast<int64_t>(c.col) * 64 + piece * 8);
+        for (int part = 0; part < kParts; ++part) {
+          // Both sets see every use of a stage, and it is ready when both have: a set that passed over the other's
+          // stages could take the phase before the last for the one it waits for.
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&full_bar[s], phase, p.status, (6u << 16) | 5u));
+          if (!ok) break;
+          if (turn == set && form)
+            form_gradient(grad.act, smem + s * stage_bytes + mine * kTileBytes + tid * 16,
+                          n0 + static_cast<uint64_t>(part * 4 * grad.number.row), step0, step1, stream, grad.drop);
+          ptx::fence_proxy_async_smem();   // the tensor core reads it through the async proxy
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&ready_bar[s]);
+          turn ^= 1;
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ok && n + 1 < my_items) c.advance(p, stride);
+      }
+      if (!ok && lane == 0) *abort_flag = 1;
     }
   } else if (warp >= 8) {
     // =========================== epilogue ===========================
@@ -460,7 +577,7 @@ bool project_umma_supported(int k, int r) { return k == 4 || ((k == 8 || k == 16
 int launch_project_umma(const void* t0, void* out0, int C0, const lbp_view* view0, const void* t1,
                         void* out1, int C1, const lbp_view* view1, int B, int H, int W,
                         const BasisPlan& bp, float scale0, float scale1, int sms, uint32_t* status,
-                        cudaStream_t stream) {
+                        cudaStream_t stream, const layer::GradOf* of) {
   using namespace umma;
   const int K = bp.k, r = bp.r;
   const int box_w = K, box_h = K == 16 ? 4 : K;
@@ -518,11 +635,12 @@ int launch_project_umma(const void* t0, void* out0, int C0, const lbp_view* view
   const int rows = r * p.per_strip, parts = K == 16 ? 4 : 1;
   const int nb = K == 4 ? (r + 3) / 4 : (r + 15) / 16;
   const int fixed = 1024 + kBarBytes + parts * (K == 4 ? 1 : nb) * 2048;
-  auto ring = [&](int groups) { return (kSmemMax - fixed - 4 * groups * rows * 128) / kStageBytes; };
-  p.groups = kMaxGroups;
+  const int stage_bytes = of != nullptr && of->z != nullptr ? 2 * kStageBytes : kStageBytes;
+  auto ring = [&](int groups) { return (kSmemMax - fixed - 4 * groups * rows * 128) / stage_bytes; };
+  p.groups = of != nullptr ? 1 : kMaxGroups;
   while (p.groups > 2 && ring(p.groups) < 4) --p.groups;
   p.stages = ring(p.groups) < kMaxStages ? ring(p.groups) : kMaxStages;
-  const int smem_bytes = fixed + p.stages * kStageBytes + 4 * p.groups * rows * 128;
+  const int smem_bytes = fixed + p.stages * stage_bytes + 4 * p.groups * rows * 128;
 
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -530,7 +648,7 @@ int launch_project_umma(const void* t0, void* out0, int C0, const lbp_view* view
   // us on 96 to 128 of 148 SMs and 45 on all, 77 MB of 14 x 14 or 56 x 56 grids in 24.6
   // us on 112, 22.6 on 128, 22.8 on all.  Beside a products kernel the caller's launch
   // shape says how many it gets.
-  const int sms_alone = projection_launch().max_ctas > 0 ? sms : (7 * sms + 7) / 8;
+  const int sms_alone = projection_launch().max_ctas > 0 || of != nullptr ? sms : (7 * sms + 7) / 8;
   const int grid = projection_grid((p.n_chunks + 3) / 4, sms_alone, attr, &cfg.numAttrs);
   for (int w = 0; w < 2; ++w) {
     const uint32_t stride = 4u * static_cast<uint32_t>(grid), np = static_cast<uint32_t>(p.cols[w]);
@@ -538,19 +656,31 @@ int launch_project_umma(const void* t0, void* out0, int C0, const lbp_view* view
     p.step[w] = Steps{stride - blk * np, blk % p.Wb, t2 % p.Hb, t2 / p.Hb};
   }
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(of != nullptr ? kThreadsOf<true> : kThreadsOf<false>);
   cfg.dynamicSmemBytes = smem_bytes;
   cfg.stream = stream;
   cfg.attrs = attr;
-  auto launch = [&](auto kern, PerDevice& configured) -> int {
+  auto launch = [&](auto kern, PerDevice& configured, const auto& grad) -> int {
     if (int e = allow_dynamic_smem(configured, reinterpret_cast<const void*>(kern), kSmemMax)) return e;
-    LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, in[0], in[1], om, p, mp));
+    LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, in[0], in[1], om, p, mp, grad));
     count_launch();
     return LBP_OK;
   };
-  static PerDevice configured[3][4];
-#define LBP_CASE(KK, NB) \
-  case KK * 10 + NB: return launch(wht_project_umma_kernel<KK, NB>, configured[KK / 8][NB - 1])
+  Grad grad{};
+  if (of != nullptr) {
+    grad.act = of->act;
+    grad.first = of->first;
+    grad.number = of->number;
+    grad.drop = of->drop;
+    grad.z = in[0];
+    if (of->z != nullptr)
+      if (int e = encode_box_tensor_map(&grad.z, of->z, LBP_BF16, B, H, W, C0, 64, box_w, box_h, true, view0)) return e;
+  }
+  static PerDevice configured[2][3][4];
+#define LBP_CASE(KK, NB)                                                                                          \
+  case KK * 10 + NB:                                                                                              \
+    return of != nullptr ? launch(wht_project_umma_kernel<KK, NB, Grad>, configured[1][KK / 8][NB - 1], grad)     \
+                         : launch(wht_project_umma_kernel<KK, NB, NoGrad>, configured[0][KK / 8][NB - 1], NoGrad{})
   switch (K * 10 + nb) {
     LBP_CASE(4, 1);
     LBP_CASE(4, 2);

@@ -574,3 +574,53 @@ def test_expired_wait_is_reported_and_the_next_call_is_clean(dev, rows, Cin, Cou
     y = lbp.lbp_linear(x, W, b, residual=res, ws=ws)
     assert lbp.lbp_poll_status(ws) == 0
     _check_linear(torch.bfloat16, y, None, _want_linear(x, W, b, "none", res, 0.0, 0, 0), 0.0)
+
+
+def test_expired_wait_in_the_projection_of_a_gradient(dev):
+    """No box is fetched: the warps that form the gradient give up too, the call reports it, the next one is right."""
+    g, z = (_normal((2, 16, 24, 256), 1.0, torch.bfloat16, s) for s in (1, 2))
+    bases = O.select_bases(8, O.RULE_PREFIX, 6)
+    ws = torch.zeros(lbp.lbp_project_grad_workspace_bytes(2, 16, 24, 256, 8, 6, lbp.LBP_BF16), dtype=torch.uint8, device=dev)
+    lbp.lbp_test_stall_products(True, projection=True)
+    try:
+        lbp.lbp_project_grad(g, z, 8, bases, activation="gelu", p=0.2, ws=ws)
+    finally:
+        lbp.lbp_test_stall_products(False)
+    assert lbp.lbp_poll_status(ws) == 10
+    got = lbp.lbp_project_grad(g, z, 8, bases, activation="gelu", p=0.2, ws=ws)
+    assert lbp.lbp_poll_status(ws) == 0
+    # the gradient is formed and rounded as lbp_linear_grad has it, and projected as lbp_project does
+    gz = lbp.lbp_linear_grad(g, z, activation="gelu", p=0.2)
+    assert torch.equal(got, lbp.lbp_project(gz, 8, bases))
+
+
+@pytest.mark.parametrize("k,H,W,r", [(4, 9, 22, 3), (4, 16, 16, 16), (8, 23, 17, 8), (8, 16, 16, 40), (16, 20, 33, 6), (16, 16, 32, 48)])
+@pytest.mark.parametrize("Cc", [8, 72, 640])
+def test_projected_gradient_is_the_projection_of_the_gradient(dev, k, H, W, r, Cc):
+    """Bit for bit: formed on the way into the projection or written out first."""
+    bases = O.select_bases(k, O.RULE_LINF if r == k * k else O.RULE_PREFIX, k if r == k * k else r)
+    g, z = _normal((5, H, W, Cc), 1.0, torch.bfloat16, 1), _normal((5, H, W, Cc), 2.0, torch.bfloat16, 2)
+    for a in ACTS:
+        for p in (0.0, 0.3, 0.7, 1.0):
+            zz = None if a == "none" else z
+            gz = lbp.lbp_linear_grad(g, zz, activation=a, p=p, seed=3, offset=4)
+            got = lbp.lbp_project_grad(g, zz, k, bases, activation=a, p=p, seed=3, offset=4)
+            assert torch.equal(got, lbp.lbp_project(gz, k, bases)), (a, p)
+
+
+def test_backward_act_without_the_mean_basis_and_on_views(dev):
+    """A list without (0, 0) cannot give the bias's sum; gradients with strides of a wider tensor; both as on the written gradient."""
+    B, H, W, Cin, Cout, k = 3, 16, 16, 128, 192, 8
+    x = _normal((B, H, W, Cin), 1.0, torch.bfloat16, 1)
+    wide = _normal((2, B, H, W, Cout + 64), 1.0, torch.bfloat16, 2)
+    g, z = wide[0, ..., 64:], wide[1, ..., 64:]
+    w = _normal((Cout, Cin), Cin ** -0.5, torch.bfloat16, 3)
+    for bases in ([(1, 0), (0, 1), (2, 2)], O.select_bases(k, O.RULE_PREFIX, 5)):
+        for bias in (False, True):
+            gb, gb2 = (torch.empty(Cout, device=dev) if bias else None for _ in range(2))
+            gx, gw = lbp.lbp_backward_act(x, g, z, w, k, bases, activation="gelu", p=0.4, seed=1, offset=8, g_bias=gb)
+            gz = lbp.lbp_linear_grad(g, z, activation="gelu", p=0.4, seed=1, offset=8)
+            rx, rw = lbp.lbp_backward_ex(x, gz, w, k, bases, g_bias=gb2)
+            assert torch.equal(gx, rx) and torch.equal(gw, rw)
+            if bias:
+                assert torch.equal(gb, gb2)
