@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int m = t / p.tiles_n;
         const int row = (m * kCtas + rank) * kBM, col = (t - m * p.tiles_n) * p.BN + rank * part;
         for (int kb = 0; kb < p.num_kb; ++kb) {
-          if (!ptx::mbar_wait(&empty[s], phase ^ 1u, p.status, kSite | 1u)) {
+          if (!ptx::mbar_wait_parked(&empty[s], phase ^ 1u, p.status, kSite | 1u)) {
             ok = false;
             break;
           }
@@ -187,12 +187,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (int t = unit; t < p.tiles && ok; t += units, ++n) {
         const uint32_t d = tmem_base + (n & 1) * kSlotCols;
-        if (!ptx::mbar_wait(&acc_empty[n & 1], ((n >> 1) + 1) & 1u, p.status, kSite | 2u)) {
+        if (!ptx::mbar_wait_parked(&acc_empty[n & 1], ((n >> 1) + 1) & 1u, p.status, kSite | 2u)) {
           ok = false;
           break;
         }
         for (int kb = 0; kb < p.num_kb; ++kb) {
-          if (!ptx::mbar_wait(&full[s], phase, p.status, kSite | 3u)) {
+          if (!ptx::mbar_wait_parked(&full[s], phase, p.status, kSite | 3u)) {
             ok = false;
             break;
           }
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool waited = false;
       auto wait = [&] {
         waited = true;
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u) &&
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_parked(&acc_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, p.status, kSite | 4u) &&
                                          *abort_flag == 0);
         ptx::tc_fence_after_sync();
       };
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
       const uint64_t keep = ptx::l2_policy_evict_last();
       for (int kb = kb0, i = 0; kb < kb1 && !p.test_stall; ++kb, ++i) {
         const int s = i % kSplitStages;
-        if (!ptx::mbar_wait(&empty[s], ((i / kSplitStages) + 1) & 1u, p.status, kSite | 7u)) break;
+        if (!ptx::mbar_wait_parked(&empty[s], ((i / kSplitStages) + 1) & 1u, p.status, kSite | 7u)) break;
         uint8_t* const sa = smem + s * stage_bytes;
         ptx::mbar_expect_tx(&full[s], stage_bytes);
         ptx::tma_load_2d_hint(sa, &tm.x, &full[s], kb * kBK, m * kBM, keep);
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
       bool ok = true;
       for (int kb = kb0, i = 0; kb < kb1 && ok; ++kb, ++i) {
         const int s = i % kSplitStages;
-        ok = ptx::mbar_wait(&full[s], (i / kSplitStages) & 1u, p.status, kSite | 8u);
+        ok = ptx::mbar_wait_parked(&full[s], (i / kSplitStages) & 1u, p.status, kSite | 8u);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         const uint32_t sa = ptx::smem_u32(smem + s * stage_bytes), sb = sa + kABytes;
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   if (warp >= 2) {
     // (a CTA without k-blocks, where they do not share out evenly, has zeros)
     bool ok = kb0 < kb1;
-    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(acc_full, 0, p.status, kSite | 9u));
+    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait_parked(acc_full, 0, p.status, kSite | 9u));
     ptx::tc_fence_after_sync();
 #pragma unroll 1
     for (int c = half * 16; c < BN; c += 32) {

@@ -79,6 +79,25 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
   return false;
 }
 
+// The same for a warp that has nothing else to do while others on its scheduler work: the hardware parks it for up to
+// 20 us at a time instead of letting it ask again and again.
+__device__ __forceinline__ bool mbar_wait_parked(uint64_t* bar, uint32_t parity, uint32_t* status, uint32_t site) {
+  const long long t0 = clock64();
+  do {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
+        : "memory");
+    if (done) return true;
+  } while (clock64() - t0 <= kWaitLimitCycles);
+  report_timeout(status, site);
+  return false;
+}
+
 // ---- proxies / fences -------------------------------------------------------
 __device__ __forceinline__ void fence_proxy_async_smem() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -57,7 +57,9 @@ constexpr int kProducers = 4;
 constexpr int kMaxGroups = 4;                    // epilogue warpgroups
 constexpr int kGradWarps = 16;                   // (GRAD, with one epilogue group)
 template <bool GRAD>
-constexpr int kThreadsOf = (8 + (GRAD ? 4 + kGradWarps : 4 * kMaxGroups)) * 32;
+constexpr int kFirstEpilogue = GRAD ? 5 : 8;     // (GRAD has no warp to spare: registers)
+template <bool GRAD>
+constexpr int kThreadsOf = (kFirstEpilogue<GRAD> + (GRAD ? 4 + kGradWarps : 4 * kMaxGroups)) * 32;
 constexpr int kMaxStages = 6;
 constexpr int kBarBytes = 256;
 constexpr int kSmemMax = 227 * 1024;
@@ -164,17 +166,16 @@ template <int ACT, bool DROP>
 __device__ __forceinline__ void form_gradient(uint8_t* at, uint64_t number, int64_t step0, int64_t step1, const layer::Stream& s,
                                               const layer::Drop& d) {
 #pragma unroll 1
-  for (int h = 0; h < 2; ++h, at += 4096, number += static_cast<uint64_t>(2 * step1)) {
-    uint32_t m[16] = {};
-    if constexpr (DROP) {   // the choices of four pieces first: eight independent chains of multiplications
-      const uint64_t group[4] = {number >> 3, (number + static_cast<uint64_t>(step0)) >> 3,
-                                 (number + static_cast<uint64_t>(step1)) >> 3, (number + static_cast<uint64_t>(step0 + step1)) >> 3};
-      layer::philox<4>(s, group, m);
+  for (int h = 0; h < 4; ++h, at += 2048, number += static_cast<uint64_t>(step1)) {
+    uint32_t m[8] = {};
+    if constexpr (DROP) {
+      const uint64_t group[2] = {number >> 3, (number + static_cast<uint64_t>(step0)) >> 3};
+      layer::philox<2>(s, group, m);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) m[j] = layer::kept_halves(m[j], d);
+      for (int j = 0; j < 8; ++j) m[j] = layer::kept_halves(m[j], d);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const uint4 g = *reinterpret_cast<const uint4*>(at + i * 1024);
       uint4 z = make_uint4(0u, 0u, 0u, 0u);
       if constexpr (ACT != LBP_ACT_NONE) z = *reinterpret_cast<const uint4*>(at + kStageBytes + i * 1024);
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
                             const __grid_constant__ OutMaps om, const __grid_constant__ Params p,
                             const __grid_constant__ MmaPlan mp, const __grid_constant__ G grad) {
   constexpr bool GRAD = std::is_same<G, Grad>::value;
-  constexpr int kThreads = kThreadsOf<GRAD>;
+  constexpr int kThreads = kThreadsOf<GRAD>, kEpi = kFirstEpilogue<GRAD>;
   constexpr int kParts = K == 16 ? 4 : 1;
   constexpr int kN = K == 4 ? 16 : NB * 16;   // columns of one MMA
   constexpr int kPanelBytes = kN * 128;       // 64 tokens x N rows
@@ -260,13 +261,13 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
   if (warp == 4) {
     ptx::tmem_alloc(tmem_slot, kTmemCols);
     ptx::tmem_relinquish();
-  } else if (warp == 5 && lane < 4) {
+  } else if (warp == 5 && lane < 4 && !GRAD) {
     ptx::prefetch_tensormap(lane == 0 ? &tmap0 : lane == 1 ? &tmap1 : &om.full[lane - 2]);
-  } else if (warp >= 8) {
+  } else if (warp >= kEpi) {
     // The basis matrix as K-major B operands, one panel per part of 64 tokens: row n = 64
     // tokens = 128 bytes, 16-byte piece c of row n at piece c ^ (n & 7); rows past the
     // bases are zero.  Order 4 uses the first 16 tokens of a row, those of a block.
-    for (int e = threadIdx.x - 256; e < kParts * kN * 8; e += kThreads - 256) {
+    for (int e = threadIdx.x - kEpi * 32; e < kParts * kN * 8; e += kThreads - kEpi * 32) {
       const int part = e / (kN * 8), n = (e >> 3) % kN, c = e & 7;
       uint32_t w[4];
 #pragma unroll
@@ -405,14 +406,14 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       }
       if (!ok) *abort_flag = 1;
     }
-  } else if (GRAD && warp >= 12) {
+  } else if (GRAD && warp >= kEpi + 4) {
     // =========================== g_z ===========================
     if constexpr (GRAD) {
       asm volatile("griddepcontrol.wait;" ::: "memory");
       const layer::Stream stream = grad.drop.on ? layer::open_stream(grad.drop) : layer::Stream{};
-      if (blockIdx.x == 0 && threadIdx.x == 12 * 32) layer::note_used(grad.drop);
+      if (blockIdx.x == 0 && threadIdx.x == (kEpi + 4) * 32) layer::note_used(grad.drop);
       // two sets of eight warps take turns on the stages, in a set two warps to a chunk
-      const int set = (warp - 12) >> 3, mine = ((warp - 12) & 7) >> 1, tid = threadIdx.x & 63;
+      const int gw = warp - (kEpi + 4), set = gw >> 3, mine = (gw & 7) >> 1, tid = (gw & 1) * 32 + lane;
       const int row = tid >> 3, piece = (tid & 7) ^ row;   // token row of the box (and 8 i on); channels 8 piece on
       const int u0 = K == 4 ? row >> 2 : 0, v0 = K == 4 ? row & 3 : row;
       const int64_t step0 = K == 8 ? grad.number.row : K == 16 ? 8 * grad.number.token : 2 * grad.number.row;
@@ -448,10 +449,10 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       }
       if (!ok && lane == 0) *abort_flag = 1;
     }
-  } else if (warp >= 8) {
+  } else if (warp >= kEpi) {
     // =========================== epilogue ===========================
     // Warpgroup g takes the CTA's items g, g + groups, ...; its warps read their lane quarter.
-    const int g = (warp - 8) >> 2, quarter = warp & 3;
+    const int g = (warp - kEpi) >> 2, quarter = warp & 3;
     const bool first = quarter == 0 && lane == 0;
     const uint64_t keep = ptx::l2_policy_evict_last();   // read back from L2 by the next kernel
     uint8_t* const out = sOut + g * 4 * out_bytes;
