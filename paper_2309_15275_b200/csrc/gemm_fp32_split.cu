@@ -132,27 +132,61 @@ __device__ __forceinline__ uint32_t take_part(float& a, float& b, int part) {
 struct NoEpilogue {};
 template <class Out>
 constexpr bool kLinear = !std::is_same<Out, NoEpilogue>::value;
-// Four channels of a token, from their product.
-__device__ __forceinline__ void emit(const NoEpilogue&, const layer::Stream&, long long, long long, float4) {}
-__device__ __forceinline__ void emit(const layer::LinearCall& p, const layer::Stream& s, long long row, long long ch, float4 sum) {
-  float v[4] = {sum.x, sum.y, sum.z, sum.w}, out[4] = {};
-  auto at = [&](const void* q, int64_t pitch) { return reinterpret_cast<float4*>(static_cast<float*>(const_cast<void*>(q)) + row * pitch + ch); };
+// Eight channels of a token (the first four where `n` is 4), from their product.
+__device__ __forceinline__ void emit(const NoEpilogue&, const layer::Stream&, long long, long long, float4, float4, int) {}
+__device__ __forceinline__ void emit(const layer::LinearCall& p, const layer::Stream& s, long long row, long long ch, float4 lo,
+                                     float4 hi, int n) {
+  float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, out[8] = {};
+  auto at = [&](const void* q, int64_t pitch) { return static_cast<float*>(const_cast<void*>(q)) + row * pitch + ch; };
+  auto read = [&](const float* from, float (&to)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(from);
+    float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (n > 4) b = *reinterpret_cast<const float4*>(from + 4);
+    to[0] = a.x, to[1] = a.y, to[2] = a.z, to[3] = a.w, to[4] = b.x, to[5] = b.y, to[6] = b.z, to[7] = b.w;
+  };
+  // (a sector in one instruction where it starts on its boundary)
+  auto write = [&](float* to, const float (&w)[8]) {
+    if (n > 4 && (reinterpret_cast<uintptr_t>(to) & 31u) == 0) {
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "f"(w[0]), "f"(w[1]), "f"(w[2]), "f"(w[3]),
+                   "f"(w[4]), "f"(w[5]), "f"(w[6]), "f"(w[7])
+                   : "memory");
+    } else {
+      *reinterpret_cast<float4*>(to) = make_float4(w[0], w[1], w[2], w[3]);
+      if (n > 4) *reinterpret_cast<float4*>(to + 4) = make_float4(w[4], w[5], w[6], w[7]);
+    }
+  };
   if (p.bias != nullptr) {
-    const float4 b = *at(p.bias, 0);
-    v[0] += b.x, v[1] += b.y, v[2] += b.z, v[3] += b.w;
-  }
-  if (p.z != nullptr) *at(p.z, p.pz) = make_float4(v[0], v[1], v[2], v[3]);
-#pragma unroll 1
-  for (int pass = 0; pass < (p.act == LBP_ACT_NONE ? 0 : 1); ++pass) {
+    float b[8];
+    read(static_cast<const float*>(p.bias) + ch, b);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = layer::act_of<false>(p.act, v[j]);
+    for (int j = 0; j < 8; ++j) v[j] += b[j];
   }
-  if (p.residual != nullptr) {
-    const float4 r = *at(p.residual, p.pr);
-    out[0] = r.x, out[1] = r.y, out[2] = r.z, out[3] = r.w;
+  if (p.z != nullptr) write(at(p.z, p.pz), v);
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) layer::act2_of<true>(p.act, v[j], v[j + 1]);
+  if (p.residual != nullptr) read(at(p.residual, p.pr), out);
+  if (p.drop.on) {
+    const uint64_t number = static_cast<uint64_t>(p.first + row * p.step + ch);
+    uint32_t w[8] = {};
+    if ((number & 4u) == 0) {
+      const uint64_t group[1] = {number >> 3};
+      uint32_t one[4];
+      layer::philox<1>(s, group, one);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = one[j];
+    } else {   // the upper half of one group and the lower of the next
+      const uint64_t group[2] = {number >> 3, (number >> 3) + 1};
+      layer::philox<2>(s, group, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = w[j + 2];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) layer::add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) out[j] += v[j];
   }
-  layer::add_dropped(out, v, static_cast<uint64_t>(p.first + row * p.step + ch), s, p.drop);
-  *at(p.y, p.py) = make_float4(out[0], out[1], out[2], out[3]);
+  write(at(p.y, p.py), out);
 }
 __device__ __forceinline__ layer::Stream stream_of(const NoEpilogue&) { return layer::Stream{}; }
 __device__ __forceinline__ layer::Stream stream_of(const layer::LinearCall& p) {
@@ -326,7 +360,7 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
                                  : i == 2 ? make_float4(v[2][0], v[2][1], v[2][2], v[2][3])
                                           : make_float4(v[3][0], v[3][1], v[3][2], v[3][3]);
           const long long row = l + h * 4 * kAlong + i;
-          if (row < item.lanes && n < item.cols) emit(epi, stream, row, n, four_of);
+          if (row < item.lanes && n < item.cols) emit(epi, stream, row, n, four_of, four_of, 4);
         }
         continue;
       }
@@ -564,10 +598,14 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
     if constexpr (LIN) {
       if (!item.planes) {
         const layer::Stream stream = stream_of(epi);
+        constexpr int kEights = kRowPieces / 2;
+        const int e = lane % kEights;
 #pragma unroll 1
-        for (int row = lane / kRowPieces; row < 32; row += 32 / kRowPieces) {
-          const long long gm = item.l0 + quarter * 32 + row, gn = n0 + 4 * c;
-          if (gm < lanes && gn < cols) emit(epi, stream, gm, gn, mine[row * kRowPieces + (c ^ (row & (kRowPieces - 1)))]);
+        for (int row = lane / kEights; row < 32; row += 32 / kEights) {
+          const long long gm = item.l0 + quarter * 32 + row, gn = n0 + 8 * e;
+          const float4* const from = mine + row * kRowPieces;
+          const int flip = row & (kRowPieces - 1);
+          if (gm < lanes && gn < cols) emit(epi, stream, gm, gn, from[(2 * e) ^ flip], from[(2 * e + 1) ^ flip], cols - gn < 8 ? 4 : 8);
         }
         return;
       }
@@ -647,7 +685,7 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const float* planes,
       const float4 v = *reinterpret_cast<const float4*>(planes + c * plane + 4 * i);
       sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
     }
-    split::emit(p, s, row, 4 * (i - row * per_row), sum);
+    split::emit(p, s, row, 4 * (i - row * per_row), sum, sum, 4);
   }
 }
 

@@ -23,7 +23,8 @@ __device__ __forceinline__ void finish_one(const LinearCall& p, const Stream& s,
   const T* const bias = static_cast<const T*>(p.bias);
   if (bias != nullptr) v += static_cast<float>(bias[ch]);
   if (p.z != nullptr) static_cast<T*>(p.z)[row * p.pz + ch] = static_cast<T>(v);
-  v = act_of<Vec<T>::kFast>(p.act, v);
+  float other = 0.f;
+  act2_of<Vec<T>::kFine>(p.act, v, other);
   float out = p.residual != nullptr ? static_cast<float>(static_cast<const T*>(p.residual)[row * p.pr + ch]) : 0.f;
   if (p.drop.on) {
     const uint64_t n = static_cast<uint64_t>(p.first + row * p.step + ch);

@@ -87,6 +87,23 @@ __device__ __forceinline__ void read16(const __nv_bfloat16* from, uint32_t (&w)[
   }
 }
 
+// Row and column of a unit's tiles, one after the other.
+struct Walk {
+  int m, n, step_m, step_n;
+  __device__ __forceinline__ Walk(const Params& p, int unit, int units) {
+    m = unit / p.tiles_n, n = unit - m * p.tiles_n;
+    step_m = units / p.tiles_n, step_n = units - step_m * p.tiles_n;
+  }
+  __device__ __forceinline__ void advance(const Params& p) {
+    m += step_m;
+    n += step_n;
+    if (n >= p.tiles_n) {
+      n -= p.tiles_n;
+      ++m;
+    }
+  }
+};
+
 template <int ACT, bool DROP, bool RES, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_umma_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
@@ -146,9 +163,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       int s = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int t = unit; t < p.tiles && ok && !p.test_stall; t += units) {
-        const int m = t / p.tiles_n;
-        const int row = (m * kCtas + rank) * kBM, col = (t - m * p.tiles_n) * p.BN + rank * part;
+      Walk at(p, unit, units);
+      for (int t = unit; t < p.tiles && ok && !p.test_stall; t += units, at.advance(p)) {
+        const int row = (at.m * kCtas + rank) * kBM, col = at.n * p.BN + rank * part;
         for (int kb = 0; kb < p.num_kb; ++kb) {
           if (!ptx::mbar_wait_parked(&empty[s], phase ^ 1u, p.status, kSite | 1u)) {
             ok = false;
@@ -227,8 +244,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int chunks = p.BN / 64;
     bool ok = true;
     int n = 0, next = e >> 2;   // chunks go round, so that every warp has as many
-    for (int t = unit; t < p.tiles && ok; t += units, ++n) {
-      const int m = t / p.tiles_n;
+    Walk at(p, unit, units);
+    for (int t = unit; t < p.tiles && ok; t += units, ++n, at.advance(p)) {
+      const int m = at.m;
       const long long row = static_cast<long long>(m * kCtas + rank) * kBM + quarter * 32 + lane;
       bool waited = false;
       auto wait = [&] {
@@ -240,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int c = next;
       static_assert(kPerQuarter >= 4, "at most one chunk of a tile a warp: the biases of a tile are written once");
       for (; c < chunks; c += kPerQuarter) {
-        const int col = (t - m * p.tiles_n) * p.BN + c * 64;
+        const int col = at.n * p.BN + c * 64;
         const int cols = p.Cout - col;                           // of this chunk on
         const int here = row < p.rows ? cols : 0;                // ... in this thread's row
         const uint32_t two_biases = p.bias != nullptr && 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
@@ -291,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             return;
           }
 #pragma unroll
-          for (int j = 0; j < 16; j += 2) act_fast<ACT>(v[j], v[j + 1]);
+          for (int j = 0; j < 16; j += 2) act2<ACT, false>(v[j], v[j + 1]);
           if constexpr (RES) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(r[j]), out[2 * j + 1] = bf16_hi(r[j]);
@@ -542,7 +560,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
         write16(p.z + grow * p.pz + col, w, left, p.wide);
       }
 #pragma unroll
-      for (int j = 0; j < 16; j += 2) act_fast<ACT>(v[j], v[j + 1]);
+      for (int j = 0; j < 16; j += 2) act2<ACT, false>(v[j], v[j + 1]);
       if constexpr (DROP) {
         const uint64_t g0 = static_cast<uint64_t>(p.first + grow * p.step + col) >> 3, group[2] = {g0, g0 + 1};
         philox<2>(stream, group, w);

@@ -695,6 +695,24 @@ bool matrix_like(const Tensor& t, const Tensor& like, at::IntArrayRef shape, int
 void* data_or_null(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 bool on_current_device(const Tensor& t) { return t.defined() && t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
 
+// A workspace for calls that need no more than a status block and whose caller has not given one, so that nobody polls
+// it: one for each device, which is written to only where a wait expires (an allocation takes a fifth of such a call).
+// Inside a stream capture a block of its own: memory of a capture's pool is the graph's.
+Tensor status_block(const Tensor& like) {
+  static std::mutex mu;
+  static auto* const blocks = new std::vector<Tensor>(64);   // (never freed: the driver may be gone at exit)
+  const int dev = like.get_device();
+  const int64_t bytes = static_cast<int64_t>(lib.status_bytes());
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  const bool free_to = dev < 64 && cudaStreamIsCapturing(c10::cuda::getCurrentCUDAStream(dev).stream(), &capture) == cudaSuccess &&
+                       capture == cudaStreamCaptureStatusNone;
+  std::lock_guard<std::mutex> lock(mu);
+  if (dev < 64 && (*blocks)[dev].defined()) return (*blocks)[dev];
+  Tensor block = fresh({bytes}, at::kByte, like);
+  if (free_to) (*blocks)[dev] = block;
+  return block;
+}
+
 struct LinearArgs {
   Tensor x, W, bias, residual, out, z, ws;
   bool save_z = false;
@@ -721,7 +739,7 @@ int run_linear(LinearArgs* c, const lbp_epilogue& e) {
   if (!c->ws.defined()) {
     const size_t bytes = lib.linear_workspace_bytes(rows, static_cast<int>(Cin), static_cast<int>(Cout), dt);
     if (bytes == 0) return -1;
-    c->ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, c->x);
+    c->ws = bytes <= lib.status_bytes() ? status_block(c->x) : fresh({static_cast<int64_t>(bytes)}, at::kByte, c->x);
   }
   if (!dense_on(c->ws, dev)) return -1;
   return lib.linear(c->x.data_ptr(), c->W.data_ptr(), data_or_null(c->bias), data_or_null(c->residual), c->out.data_ptr(),
