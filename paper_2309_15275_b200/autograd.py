@@ -50,6 +50,8 @@ class LbpLinear(torch.nn.Module):
     condition: no graph of earlier, uncaptured passes over the same parameters is alive.
     """
 
+    activation, dropout = None, 0.0     # (also of modules stored before there were these)
+
     def __init__(self, in_features: int, out_features: int, k: int,
                  bases: Sequence[Tuple[int, int]], device=None, dtype=None, bias: bool = False,
                  save_projected: bool = False, grid=None, activation=None, dropout: float = 0.0):

@@ -61,16 +61,22 @@ static Drop drop_of(const lbp_epilogue& e) {
   return d;
 }
 
-// The bytes of `rows` rows at p.
+// The bytes of `rows` rows at p: runs of `width`, `pitch` apart, from lo to hi.
 struct Range {
-  uintptr_t lo, hi;
+  uintptr_t lo, hi, width, pitch;
 };
 static Range range(const void* p, long long rows, int64_t pitch, int C, int dtype) {
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  if (p == nullptr || rows == 0) return Range{0, 0};
-  return Range{lo, lo + (static_cast<uintptr_t>(rows - 1) * pitch + C) * elem_size(dtype)};
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p), es = elem_size(dtype);
+  if (p == nullptr || rows == 0) return Range{};
+  return Range{lo, lo + (static_cast<uintptr_t>(rows - 1) * pitch + C) * es, C * es, static_cast<uintptr_t>(pitch) * es};
 }
-static bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+static bool overlap(const Range& a, const Range& b) {
+  if (a.lo >= b.hi || b.lo >= a.hi) return false;
+  if (a.pitch != b.pitch || a.pitch == 0) return true;
+  // columns of one wide matrix: how far b's runs start behind a's
+  const uintptr_t behind = b.lo >= a.lo ? (b.lo - a.lo) % a.pitch : (a.pitch - (a.lo - b.lo) % a.pitch) % a.pitch;
+  return behind < a.width || behind + b.width > a.pitch;
+}
 
 static lbp_view rows_at(int64_t pitch) { return lbp_view{pitch, 0, 0}; }
 
@@ -223,7 +229,7 @@ int lbp_linear(const void* x, const void* W, const void* bias, const void* resid
   if (overlap(out[0], out[1])) return LBP_ERR_OVERLAP;
   const size_t need = lbp_linear_workspace_bytes(rows, Cin, Cout, dtype);
   if (ws == nullptr || ws_bytes < need) return LBP_ERR_WORKSPACE;
-  const Range scratch{reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + need};
+  const Range scratch{reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + need, need, 0};
   for (const Range& q : {out[0], out[1], in[0], in[1], in[2], in[3]})
     if (overlap(scratch, q)) return LBP_ERR_OVERLAP;
   if (int s = check_device_arch()) return s;

@@ -624,3 +624,41 @@ def test_backward_act_without_the_mean_basis_and_on_views(dev):
             assert torch.equal(gx, rx) and torch.equal(gw, rw)
             if bias:
                 assert torch.equal(gb, gb2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [5, 300])
+def test_all_tensors_in_columns_of_one_matrix(dev, dtype, rows):
+    Cin, Cout = 64, 96
+    wide = _normal((rows, Cin + 3 * Cout), 1.0, dtype, 1)
+    x, r, y, z = wide[:, :Cin], *(wide[:, Cin + i * Cout:Cin + (i + 1) * Cout] for i in range(3))
+    _, W, b = _inputs(rows, Cin, Cout, dtype, 2)
+    before = wide.clone()
+    ry, rz = lbp.lbp_linear(x.contiguous(), W, b, activation="gelu", residual=r.contiguous(), p=0.2, seed=1, save_z=True)
+    lbp.lbp_linear(x, W, b, activation="gelu", residual=r, p=0.2, seed=1, out=y, z=z)
+    assert torch.equal(y, ry) and torch.equal(z, rz) and torch.equal(wide[:, :Cin + Cout], before[:, :Cin + Cout])
+    want = lbp.lbp_linear_grad(ry, rz, activation="gelu", p=0.2, seed=1)
+    lbp.lbp_linear_grad(y, z, activation="gelu", p=0.2, seed=1, out=r)
+    assert torch.equal(r, want) and torch.equal(wide[:, :Cin], before[:, :Cin])
+
+
+def test_a_module_stored_without_an_epilogue_loads(dev, tmp_path):
+    layer = lbp.LbpLinear(64, 32, 8, [(0, 0)], device=dev, dtype=torch.bfloat16)
+    del layer.__dict__["activation"], layer.__dict__["dropout"]
+    torch.save(layer, tmp_path / "layer.pt")
+    back = torch.load(tmp_path / "layer.pt", weights_only=False)
+    x = _normal((1, 8, 8, 64), 1.0, torch.bfloat16, 1)
+    assert torch.equal(back(x), layer(x))
+
+
+def test_dropout_repeats_under_checkpointing(dev):
+    """torch's checkpoint puts the generator back for the second forward pass: the same elements are dropped."""
+    from torch.utils.checkpoint import checkpoint
+    layer = lbp.LbpLinear(64, 64, 8, O.select_bases(8, O.RULE_PREFIX, 64), device=dev, dtype=torch.float32, activation="silu", dropout=0.4)
+    x = _normal((2, 8, 8, 64), 1.0, torch.float32, 1).requires_grad_()
+    grads = []
+    for run in (lambda: layer(layer(x)), lambda: checkpoint(lambda v: layer(layer(v)), x, use_reentrant=False)):
+        torch.manual_seed(3)
+        y = run()
+        grads.append(torch.autograd.grad(y.square().sum(), (x, layer.weight)))
+    assert all(torch.equal(a, b) for a, b in zip(*grads))

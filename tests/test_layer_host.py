@@ -188,6 +188,21 @@ def test_structs_of_the_epilogue_have_the_librarys_layout():
         assert lib.lbp_test_struct_size(which) == C.sizeof(cls), cls.__name__
 
 
+@pytest.mark.parametrize("want,more", [
+    # columns of one wide matrix (pitch 160 elements of 2 bytes): x 0..63, y 64..95, z 96..127
+    (None, dict(y=P + 128, z=P + 192, pitch=B.Pitches(x=160, y=160, z=160))),
+    # the residual ahead of y in the rows, one row further on
+    (None, dict(y=P + 128 + 320, residual=P + 256, pitch=B.Pitches(x=160, y=160, residual=160))),
+    (OVERLAP, dict(y=P + 112, pitch=B.Pitches(x=160, y=160))),                      # into x's columns
+    (OVERLAP, dict(y=P + 288, pitch=B.Pitches(x=160, y=160))),                      # into the next row's
+    (OVERLAP, dict(y=P + 128, z=P + 176, pitch=B.Pitches(x=160, y=160, z=160))),    # into y's
+    (OVERLAP, dict(y=P + 128, pitch=B.Pitches(x=160, y=320))),                      # another distance: not looked into
+])
+def test_columns_of_one_matrix_are_apart(want, more):
+    # (accepted: what is left to fail is the machine without a device)
+    assert _linear(**more) in ((8, 9) if want is None else (want,))
+
+
 def test_binding_refuses_on_the_cpu_and_names_the_error():
     x, W = torch.zeros(3, 64), torch.zeros(32, 64)
     with pytest.raises(ValueError, match="CUDA"):
