@@ -10,14 +10,15 @@
 // Warps: 0 TMA loads, 1 tcgen05, 2-17 the epilogue, four to each quarter of the accumulator's lanes, which
 // take turns on its chunks of 64 columns.  Such a warp works alone on its 32 tokens x 64 channels, 16 channels at a
 // time.  A thread has a token, so that its channels lie together and one Philox call serves eight of them.  The
-// results go to a box in shared memory and out by TMA, which clips what hangs over the last token and channel; z in a
-// pass of its own ahead of y's, through the same box.  The residual is read 32 bytes (a sector) a thread.
+// results go to a box in shared memory and out by TMA, which clips what hangs over the last token and channel: y of 64
+// channels, or z and y of 32.  The residual is read 32 bytes (a sector) a thread.
 //
 // What bounds it, at 32768 tokens 768 -> 3072 and 1965 MHz: the operands' way from L2 (1.2 GB: 93 us without any
-// store, 1.66 PFLOP/s), which the stores share (y 22 us, z 27), and with GELU and dropout the epilogue's arithmetic
-// (31 instructions an element with z).  Tried: a 32-byte store a thread (no shared memory, six stages: 112, z
-// 149, all 175 us, 48 -> 192 channels 46 instead of 43), a bulk copy per row by its thread (116 and 201), twelve warps
-// (116, 142, 185).
+// store, 1.66 PFLOP/s), which the stores share (y 112, z too 135), and with GELU and dropout the epilogue's arithmetic
+// (26 instructions an element; 151); long runs the power cap (175 at 1.4 GHz).  Tried before the arithmetic was what it
+// is now, against 116, 144 and 171 us: a 32-byte store a thread without shared memory (112, 149, 175, and 48 -> 192
+// channels 46 instead of 43), a bulk copy per row by its thread (116, 201, 297), twelve warps (116, 142, 185).  z
+// in a pass of its own: 139 and 155 now, 48 -> 192 channels 40 instead of 37, GELU without dropout 134 instead of 138.
 #include "layer_math.cuh"
 #include "ptx_sm100.cuh"
 
@@ -104,7 +105,7 @@ struct Walk {
   }
 };
 
-template <int ACT, bool DROP, bool RES, bool PAIR>
+template <int ACT, bool DROP, bool RES, bool ZY, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_umma_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   constexpr int kCtas = PAIR ? 2 : 1;
@@ -238,7 +239,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     // =========================== epilogue ===========================
     const int e = warp - 2, quarter = warp & 3;
     uint8_t* const box = outs + e * kBoxBytes;
-    uint8_t* const mine = box + lane * 128;
     const Stream stream = DROP ? open_stream(p.drop) : Stream{};
     if (blockIdx.x == 0 && warp == 2 && lane == 0) note_used(p.drop);
     const int chunks = p.BN / 64;
@@ -274,25 +274,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         const uint32_t acc = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kSlotCols + c * 64;
         const uint64_t number = static_cast<uint64_t>(p.first + row * p.step + col);
-        auto put_words = [&](int h, const uint32_t (&w)[8]) {
-          if (h == 0) {
-            if (lane == 0) bulk_wait_read();   // the box has been sent
-            __syncwarp();
+        // y of 64 channels takes the whole box, in the 128-byte swizzle; z and y of 32 a half each, in the 64-byte one
+        auto put = [&](bool first_half, int h, const uint32_t (&w)[8]) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            uint8_t* const to = ZY ? box + (first_half ? 0 : kBoxBytes / 2) + lane * 64 + ((((h & 1) * 2 + g) ^ ((lane >> 1) & 3)) << 4)
+                                   : box + lane * 128 + (((h * 2 + g) ^ (lane & 7)) << 4);
+            *reinterpret_cast<uint4*>(to) = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
           }
-#pragma unroll
-          for (int g = 0; g < 2; ++g)
-            *reinterpret_cast<uint4*>(mine + (((h * 2 + g) ^ (lane & 7)) << 4)) =
-                make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
-        };
-        auto put = [&](int h, const float (&o)[16]) {
-          uint32_t w[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(o[2 * j], o[2 * j + 1]);
-          put_words(h, w);
         };
         // 16 channels at h * 16, from the accumulator in a
-        auto step = [&](auto is_z, int h, const uint32_t (&a)[16]) {
-          constexpr bool Z = decltype(is_z)::value;
+        auto step = [&](int h, const uint32_t (&a)[16]) {
           float v[16], out[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(a[j]);
@@ -304,9 +296,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           const int left = here - h * 16;
           uint32_t w[8];
-          if (Z) {
-            put(h, v);
-            return;
+          uint32_t zw[8];
+          if constexpr (ZY) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) zw[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
           }
 #pragma unroll
           for (int j = 0; j < 16; j += 2) act2<ACT, false>(v[j], v[j + 1]);
@@ -315,61 +308,72 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < 8; ++j) out[2 * j] = bf16_lo(r[j]), out[2 * j + 1] = bf16_hi(r[j]);
             if (h < 3) read16(res + (h + 1) * 16, r, left - 16, p.wide);
           }
-          if constexpr (DROP && !RES) {   // what is dropped is cleared in the packed result
+          if constexpr (DROP) {
             const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
             philox<2>(stream, group, w);
+          }
+          if constexpr (DROP && !RES) {   // what is dropped is cleared in the packed result
 #pragma unroll
             for (int j = 0; j < 16; j += 2) parts(mul2(two(v[j], v[j + 1]), two(p.drop.scale)), v[j], v[j + 1]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]) & kept_halves(w[j], p.drop);
-            put_words(h, w);
-            return;
-          } else if constexpr (DROP) {
-            const uint64_t g0 = (number >> 3) + h * 2, group[2] = {g0, g0 + 1};
-            philox<2>(stream, group, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
-          } else if constexpr (RES) {
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) parts(add2(two(out[j], out[j + 1]), two(v[j], v[j + 1])), out[j], out[j + 1]);
           } else {
+            if constexpr (DROP) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) out[j] = v[j];
+              for (int j = 0; j < 8; ++j) add_kept2(out[2 * j], out[2 * j + 1], v[2 * j], v[2 * j + 1], w[j], p.drop);
+            } else if constexpr (RES) {
+#pragma unroll
+              for (int j = 0; j < 16; j += 2) parts(add2(two(out[j], out[j + 1]), two(v[j], v[j + 1])), out[j], out[j + 1]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) out[j] = v[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(out[2 * j], out[2 * j + 1]);
           }
-          put(h, out);
+          if (h == 0 || (ZY && h == 2)) {
+            if (lane == 0) bulk_wait_read();   // what the box held has been sent
+            __syncwarp();
+          }
+          if constexpr (ZY) put(true, h, zw);
+          put(false, h, w);
         };
-        auto pass = [&](auto is_z, const CUtensorMap& map) {
-          uint32_t a0[16];
-          if constexpr (DROP && RES) {   // (the registers are needed otherwise)
-#pragma unroll 1
-            for (int h = 0; h < 4; ++h) {
-              ptx::tmem_ld_32x16(acc + h * 16, a0);
-              ptx::tmem_ld_wait();
-              step(is_z, h, a0);
-            }
-          } else {   // a step's accumulator is read while the one before is worked on
-            uint32_t a1[16];
-            ptx::tmem_ld_32x16(acc, a0);
-            ptx::tmem_ld_wait();
-#pragma unroll 1
-            for (int h = 0; h < 4; h += 2) {
-              ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
-              step(is_z, h, a0);
-              ptx::tmem_ld_wait();
-              if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
-              step(is_z, h + 1, a1);
-              ptx::tmem_ld_wait();
-            }
-          }
+        auto send = [&](int from) {   // the box, whose channels begin `from` further on
           ptx::fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (cols > 0 && row < p.rows) store_2d(&map, box, col, static_cast<int32_t>(row));
+            if (col + from < p.Cout && row < p.rows) {
+              if constexpr (ZY) store_2d(&tm.z, box, col + from, static_cast<int32_t>(row));
+              store_2d(&tm.y, ZY ? box + kBoxBytes / 2 : box, col + from, static_cast<int32_t>(row));
+            }
             bulk_commit();
           }
         };
-        if (p.z != nullptr) pass(std::true_type{}, tm.z);
-        pass(std::false_type{}, tm.y);
+        uint32_t a0[16];
+        if constexpr (DROP && RES) {   // (the registers are needed otherwise)
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            ptx::tmem_ld_32x16(acc + h * 16, a0);
+            ptx::tmem_ld_wait();
+            step(h, a0);
+            if (ZY && h == 1) send(0);
+          }
+        } else {   // a step's accumulator is read while the one before is worked on
+          uint32_t a1[16];
+          ptx::tmem_ld_32x16(acc, a0);
+          ptx::tmem_ld_wait();
+#pragma unroll 1
+          for (int h = 0; h < 4; h += 2) {
+            ptx::tmem_ld_32x16(acc + (h + 1) * 16, a1);
+            step(h, a0);
+            ptx::tmem_ld_wait();
+            if (h == 0) ptx::tmem_ld_32x16(acc + 32, a0);
+            step(h + 1, a1);
+            ptx::tmem_ld_wait();
+            if (ZY && h == 0) send(0);
+          }
+        }
+        send(ZY ? 32 : 0);
       }
       next = c - chunks;
       if (!waited) wait();
@@ -673,9 +677,9 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   if (int e = encode_matrix_tensor_map(&tm.W, c.W, c.Cout, c.Cin, part)) return e;
   tm.y = tm.z = tm.x;
   if (plan.split == 1)   // (else by plain stores)
-    if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py)) return e;
+    if (int e = encode_matrix_tensor_map(&tm.y, c.y, c.rows, c.Cout, 32, c.py, c.z != nullptr ? 32 : 64)) return e;
   if (plan.split == 1 && c.z != nullptr)
-    if (int e = encode_matrix_tensor_map(&tm.z, c.z, c.rows, c.Cout, 32, c.pz)) return e;
+    if (int e = encode_matrix_tensor_map(&tm.z, c.z, c.rows, c.Cout, 32, c.pz, 32)) return e;
 
   const int units = plan.pair ? sms / 2 : sms;
   cudaLaunchConfig_t cfg = {};
@@ -713,16 +717,19 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
       return c.drop.on ? launch(linear_split_kernel<ACT, true, 4>, split_configured[3])
                        : launch(linear_split_kernel<ACT, false, 4>, split_configured[2]);
     }
-    static PerDevice configured[8];
-    auto by = [&](auto drop, auto res) -> int {
-      constexpr bool DROP = decltype(drop)::value, RES = decltype(res)::value;
-      PerDevice* const d = configured + 2 * (2 * DROP + RES);
-      return plan.pair ? launch(linear_umma_kernel<ACT, DROP, RES, true>, d[1])
-                       : launch(linear_umma_kernel<ACT, DROP, RES, false>, d[0]);
+    static PerDevice configured[16];
+    auto by = [&](auto drop, auto res, auto zy) -> int {
+      constexpr bool DROP = decltype(drop)::value, RES = decltype(res)::value, ZY = decltype(zy)::value;
+      PerDevice* const d = configured + 2 * (4 * DROP + 2 * RES + ZY);
+      return plan.pair ? launch(linear_umma_kernel<ACT, DROP, RES, ZY, true>, d[1])
+                       : launch(linear_umma_kernel<ACT, DROP, RES, ZY, false>, d[0]);
+    };
+    auto by_z = [&](auto drop, auto res) -> int {
+      return c.z != nullptr ? by(drop, res, std::true_type{}) : by(drop, res, std::false_type{});
     };
     if (c.drop.on)
-      return c.residual != nullptr ? by(std::true_type{}, std::true_type{}) : by(std::true_type{}, std::false_type{});
-    return c.residual != nullptr ? by(std::false_type{}, std::true_type{}) : by(std::false_type{}, std::false_type{});
+      return c.residual != nullptr ? by_z(std::true_type{}, std::true_type{}) : by_z(std::true_type{}, std::false_type{});
+    return c.residual != nullptr ? by_z(std::false_type{}, std::true_type{}) : by_z(std::false_type{}, std::false_type{});
   });
 }
 

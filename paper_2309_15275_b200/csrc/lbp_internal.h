@@ -116,9 +116,9 @@ inline lbp_view resolve_view(const lbp_view* v, int H, int W, int C) {
 }
 inline bool is_dense(const lbp_view* v) { return v == nullptr || v->token == 0; }
 // 2-D row-major bf16 matrix (rows, cols): box = box_rows x 64 columns (128 B),
-// 128-byte swizzle.  pitch: elements between rows (0: dense).
+// 128-byte swizzle, or x 32 (64 B) and the 64-byte one.  pitch: elements between rows (0: dense).
 int encode_matrix_tensor_map(CUtensorMap* map, const void* base, long long rows, long long cols,
-                             int box_rows, long long pitch = 0);
+                             int box_rows, long long pitch = 0, int box_cols = 64);
 
 // 2-D row-major fp32 matrix (rows, cols), no swizzle, or the 128-byte one (boxes of 32 columns).  pitch: elements
 // between rows (0: dense).

@@ -57,7 +57,7 @@ constexpr int kProducers = 4;
 constexpr int kMaxGroups = 4;                    // epilogue warpgroups
 constexpr int kGradWarps = 16;                   // (GRAD, with one epilogue group)
 template <bool GRAD>
-constexpr int kFirstEpilogue = GRAD ? 5 : 8;     // (GRAD has no warp to spare: registers)
+constexpr int kFirstEpilogue = GRAD ? 3 : 8;     // (GRAD has no warp to spare: registers)
 template <bool GRAD>
 constexpr int kThreadsOf = (kFirstEpilogue<GRAD> + (GRAD ? 4 + kGradWarps : 4 * kMaxGroups)) * 32;
 constexpr int kMaxStages = 6;
@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
                             const __grid_constant__ MmaPlan mp, const __grid_constant__ G grad) {
   constexpr bool GRAD = std::is_same<G, Grad>::value;
   constexpr int kThreads = kThreadsOf<GRAD>, kEpi = kFirstEpilogue<GRAD>;
+  constexpr int kProd = GRAD ? 2 : kProducers, kMma = kProd;   // producer warps; the issuer's
   constexpr int kParts = K == 16 ? 4 : 1;
   constexpr int kN = K == 4 ? 16 : NB * 16;   // columns of one MMA
   constexpr int kPanelBytes = kN * 128;       // 64 tokens x N rows
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
   // 192 -> 48 with 200704 tokens 95.8 -> 94.4).
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      ptx::mbar_init(&full_bar[s], kProducers);
+      ptx::mbar_init(&full_bar[s], kProd);
       ptx::mbar_init(&empty_bar[s], 1);
       if constexpr (GRAD) ptx::mbar_init(&ready_bar[s], kGradWarps);
     }
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
     ptx::mbar_fence_init();
     *abort_flag = 0;
   }
-  if (warp == 4) {
+  if (warp == kMma) {
     ptx::tmem_alloc(tmem_slot, kTmemCols);
     ptx::tmem_relinquish();
   } else if (warp == 5 && lane < 4 && !GRAD) {
@@ -290,8 +291,8 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
   // read the buffers written below: nothing is read or written before it has
   // completed, unless the caller vouches for disjoint buffers (then the wait
   // moves to the end and only keeps completion ordered)
-  if (warp < kProducers) {
-    group_sync(1 + kMaxGroups);
+  if (warp < kProd) {
+    asm volatile("bar.sync %0, %1;" ::"n"(1 + kMaxGroups), "n"(kProd * 32) : "memory");
     asm volatile("bar.arrive %0, %1;" ::"r"(2 + kMaxGroups), "n"(kThreads) : "memory");
     if (!p.defer_wait) asm volatile("griddepcontrol.wait;" ::: "memory");
     // A kernel launched behind this one the same way may set itself up as SMs free up; it
@@ -303,14 +304,14 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
     asm volatile("bar.sync %0, %1;" ::"r"(2 + kMaxGroups), "n"(kThreads) : "memory");
     ptx::tc_fence_after_sync();
   }
-  const uint32_t tmem_base = warp < kProducers ? 0u : *tmem_slot;
+  const uint32_t tmem_base = warp < kProd ? 0u : *tmem_slot;
 
   // items dealt to the CTAs round robin
   const uint32_t n_items = (p.n_chunks + 3) / 4;
   const uint32_t my_items = blockIdx.x < n_items ? (n_items - blockIdx.x + gridDim.x - 1) / gridDim.x : 0u;
   const uint32_t stride = 4u * gridDim.x;   // chunks between a CTA's consecutive items
 
-  if (warp < kProducers) {
+  if (warp < kProd) {
     // =========================== TMA producers ===========================
     // One 8 KB box per chunk, each from a warp of its own: a thread issues TMA
     // requests too slowly to fetch an item alone.
@@ -318,49 +319,58 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       // x and g_y are read exactly once: they should not push the coefficients
       // just written (read back from L2 by the next kernel) out of L2
       const uint64_t stream_once = ptx::l2_policy_evict_first();
-      Cursor c;
-      c.decode(p, 4 * blockIdx.x + warp);
+      constexpr int kMine = kProducers / kProd;   // chunks of an item: warp, warp + kProd
+      Cursor cs[kMine];
+#pragma unroll
+      for (int q = 0; q < kMine; ++q) cs[q].decode(p, 4 * blockIdx.x + warp + q * kProd);
       bool ok = true;
       int s = 0;
       uint32_t phase = 0;
       for (uint32_t n = 0; n < my_items && !p.test_stall && ok; ++n) {
-        const int ch = static_cast<int>(c.col) * 64;
-        const bool have = c.chunk < p.n_chunks;
         for (int part = 0; part < kParts; ++part) {
           if (!ptx::mbar_wait(&empty_bar[s], phase ^ 1u, p.status, (6u << 16) | 1u)) {
             ok = false;
             break;
           }
-          if (have) {
-            // the whole box counts, also where it hangs over the tensor (zero fill)
-            const bool z_too = with_z && c.which == 0;
-            ptx::mbar_expect_tx(&full_bar[s], z_too ? 2 * kTileBytes : kTileBytes);
+          // the whole box counts, also where it hangs over the tensor (zero fill)
+          uint32_t bytes = 0;
+#pragma unroll
+          for (int q = 0; q < kMine; ++q)
+            if (cs[q].chunk < p.n_chunks) bytes += with_z && cs[q].which == 0 ? 2 * kTileBytes : kTileBytes;
+          if (bytes > 0)
+            ptx::mbar_expect_tx(&full_bar[s], bytes);
+          else
+            ptx::mbar_arrive(&full_bar[s]);   // no such chunk: what lies in the stage is multiplied and dropped
+#pragma unroll
+          for (int q = 0; q < kMine; ++q) {
+            const Cursor& c = cs[q];
+            if (c.chunk >= p.n_chunks) continue;
             constexpr int kBoxes = K == 4 ? 4 : 1;
             auto fetch = [&](const CUtensorMap* map, uint8_t* to) {
 #pragma unroll
               for (int j = 0; j < kBoxes; ++j)
-                ptx::tma_load_4d_hint(to + warp * kTileBytes + j * (kTileBytes / kBoxes), map, &full_bar[s], ch,
-                                      static_cast<int32_t>(c.bw * kBoxW) + j * 4,
+                ptx::tma_load_4d_hint(to + (warp + q * kProd) * kTileBytes + j * (kTileBytes / kBoxes), map, &full_bar[s],
+                                      static_cast<int32_t>(c.col) * 64, static_cast<int32_t>(c.bw * kBoxW) + j * 4,
                                       static_cast<int32_t>(c.bh * (K == 16 ? 16 : kBoxH) + part * 4),
                                       static_cast<int32_t>(c.b), stream_once);
             };
             fetch(c.which ? &tmap1 : &tmap0, smem + s * stage_bytes);
             if constexpr (GRAD) {
-              if (z_too) fetch(&grad.z, smem + s * stage_bytes + kStageBytes);
+              if (with_z && c.which == 0) fetch(&grad.z, smem + s * stage_bytes + kStageBytes);
             }
-          } else {
-            ptx::mbar_arrive(&full_bar[s]);   // no such chunk: what lies in the stage is multiplied and dropped
           }
           if (++s == p.stages) {
             s = 0;
             phase ^= 1u;
           }
         }
-        if (ok && n + 1 < my_items) c.advance(p, stride);
+#pragma unroll
+        for (int q = 0; q < kMine; ++q)
+          if (ok && n + 1 < my_items) cs[q].advance(p, stride);
       }
       if (!ok) *abort_flag = 1;
     }
-  } else if (warp == 4) {
+  } else if (warp == kMma) {
     // =========================== tcgen05 issuer ===========================
     if (ptx::elect_one()) {
       constexpr uint32_t idesc = ptx::idesc_bf16(128, kN, true, false);
@@ -539,7 +549,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
 
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (warp == 4) {
+  if (warp == kMma) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tmem_base, kTmemCols);
   }
