@@ -254,8 +254,9 @@ __device__ __forceinline__ void act2_of(int a, float& z0, float& z1) {
 template <int ACT, bool FINE>
 __device__ __forceinline__ void times_slope2(float& g0, float& g1, float z0, float z1) {
   if constexpr (ACT == LBP_ACT_RELU) {
-    g0 = z0 > 0.f ? g0 : z0 <= 0.f ? 0.f : z0;   // (NaN stays)
-    g1 = z1 > 0.f ? g1 : z1 <= 0.f ? 0.f : z1;
+    const float a = at_least(z0, 0.f), b = at_least(z1, 0.f);
+    g0 = a > 0.f ? g0 : a;   // (0, or NaN)
+    g1 = b > 0.f ? g1 : b;
   } else if constexpr (ACT == LBP_ACT_GELU) {
     // Phi(z) + z phi(z) = 1/2 + sign(z) d, d = 1/2 - exp(-a^2/2) (Q - a / sqrt(2 pi)) >= 0, a = |z|
     const F2 a = two(at_most(fabsf(z0), 100.f), at_most(fabsf(z1), 100.f));

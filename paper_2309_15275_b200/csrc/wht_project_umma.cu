@@ -208,6 +208,12 @@ struct OutMaps {
   CUtensorMap full[2], tail[2];
 };
 
+template <bool PARKED>
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, uint32_t* status, uint32_t site) {
+  if constexpr (PARKED) return ptx::mbar_wait_parked(bar, parity, status, site);
+  return ptx::mbar_wait(bar, parity, status, site);
+}
+
 // K: order; NB: N / 16 (order 4: what the epilogue reads of a block's 16 columns, / 4)
 template <int K, int NB, class G>
 __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
@@ -328,7 +334,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       uint32_t phase = 0;
       for (uint32_t n = 0; n < my_items && !p.test_stall && ok; ++n) {
         for (int part = 0; part < kParts; ++part) {
-          if (!ptx::mbar_wait(&empty_bar[s], phase ^ 1u, p.status, (6u << 16) | 1u)) {
+          if (!wait<GRAD>(&empty_bar[s], phase ^ 1u, p.status, (6u << 16) | 1u)) {
             ok = false;
             break;
           }
@@ -381,12 +387,12 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       for (uint32_t n = 0; n < my_items && ok; ++n) {
         const int slot = static_cast<int>(n % kSlots);
         const bool second = 4 * (blockIdx.x + n * gridDim.x) + 2 < p.n_chunks;   // of the two halves of an item
-        if (!ptx::mbar_wait(&acc_empty[slot], ((n / kSlots) + 1) & 1u, p.status, (6u << 16) | 2u)) {
+        if (!wait<GRAD>(&acc_empty[slot], ((n / kSlots) + 1) & 1u, p.status, (6u << 16) | 2u)) {
           ok = false;
           break;
         }
         for (int part = 0; part < kParts; ++part) {
-          if (!ptx::mbar_wait(GRAD ? &ready_bar[s] : &full_bar[s], phase, p.status, (6u << 16) | 3u)) {
+          if (!wait<GRAD>(GRAD ? &ready_bar[s] : &full_bar[s], phase, p.status, (6u << 16) | 3u)) {
             ok = false;
             break;
           }
@@ -441,7 +447,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
         for (int part = 0; part < kParts; ++part) {
           // Both sets see every use of a stage, and it is ready when both have: a set that passed over the other's
           // stages could take the phase before the last for the one it waits for.
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&full_bar[s], phase, p.status, (6u << 16) | 5u));
+          ok = __all_sync(0xffffffffu, wait<GRAD>(&full_bar[s], phase, p.status, (6u << 16) | 5u));
           if (!ok) break;
           if (turn == set && form)
             form_gradient(grad.act, smem + s * stage_bytes + mine * kTileBytes + tid * 16,
@@ -468,7 +474,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
     uint8_t* const out = sOut + g * 4 * out_bytes;
     for (uint32_t n = g < p.groups ? g : my_items; n < my_items; n += p.groups) {
       const int slot = static_cast<int>(n % kSlots);
-      const bool ok = ptx::mbar_wait(&acc_full[slot], (n / kSlots) & 1u, p.status, (6u << 16) | 4u);
+      const bool ok = wait<GRAD>(&acc_full[slot], (n / kSlots) & 1u, p.status, (6u << 16) | 4u);
       // the stores of the group's last item have read its buffer
       if (quarter == 0) bulk_wait_read();
       // one answer for the whole group (the flag may be raised between two reads of it)
