@@ -311,7 +311,8 @@ int lbp_backward_fullrank(const void* x, const void* g_y, const void* W,
  *
  * A row has C elements; `pitch` arguments are distances between rows in elements
  * (0: dense rows, C), at least C and with the same alignment as pointers.  Rows of
- * one tensor may not overlap.  rows = 0 is a call that does nothing. */
+ * one tensor may not overlap.  rows = 0 is a call that does nothing.  A row has at most
+ * 2^30 elements and a grid fewer than 2^31 tokens an image (LBP_ERR_SHAPE). */
 typedef enum {
   LBP_ACT_NONE = 0,
   LBP_ACT_RELU = 1,       /* act'(0) = 0                                        */
@@ -331,7 +332,8 @@ typedef struct {
   const uint64_t* seed_dev;
   const uint64_t* offset_dev;
   /* NULL, or a DEVICE array of two: the seed and offset that the call has used
-   * are written there (for the seed_dev and offset_dev of its backward pass). */
+   * are written there (for the seed_dev and offset_dev of its backward pass).  It may
+   * hold neither *seed_dev nor *offset_dev of the same call (LBP_ERR_OVERLAP). */
   uint64_t* used;
   /* Number of an element: of element c of row i, first + i * number.token + c; of
    * element (b, h, w, c) of a token grid, first + b * number.image + h * number.row +

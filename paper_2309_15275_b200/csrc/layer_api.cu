@@ -19,7 +19,7 @@ constexpr int64_t kMostElements = int64_t{1} << 62;
 
 static int check_rows(long long rows, int C, int dtype) {
   if (dtype != LBP_F32 && dtype != LBP_BF16) return LBP_ERR_DTYPE;
-  if (rows < 0 || rows > (1ll << 40) || C <= 0) return LBP_ERR_SHAPE;
+  if (rows < 0 || rows > (1ll << 40) || C <= 0 || C > (1 << 30)) return LBP_ERR_SHAPE;
   if ((static_cast<long long>(C) * elem_size(dtype)) % 16 != 0) return LBP_ERR_ALIGN;
   return LBP_OK;
 }
@@ -40,6 +40,9 @@ static int check_epilogue(const lbp_epilogue& e, int dtype) {
   if (((reinterpret_cast<uintptr_t>(e.seed_dev) | reinterpret_cast<uintptr_t>(e.offset_dev) |
         reinterpret_cast<uintptr_t>(e.used)) & 7u) != 0)
     return LBP_ERR_ALIGN;
+  // (one thread writes it while others still read)
+  for (const uint64_t* q : {e.seed_dev, e.offset_dev})
+    if (e.used != nullptr && (q == e.used || q == e.used + 1)) return LBP_ERR_OVERLAP;
   return LBP_OK;
 }
 
@@ -121,9 +124,12 @@ static int check_pointwise(const void* a, const void* b, bool need_b, const void
   return bad(a, pa) || bad(b, pb) ? LBP_ERR_OVERLAP : LBP_OK;
 }
 
+// Whether a token's place in its image has 31 bits.
+static bool fits_grid(int H, int W) { return static_cast<long long>(H) * W < (1ll << 31); }
 static int check_shape(int B, int H, int W, int C, int k, int dtype) {
   if (int s = check_order(k)) return s;
   if (B <= 0 || H <= 0 || W <= 0) return LBP_ERR_SHAPE;
+  if (!fits_grid(H, W)) return LBP_ERR_SHAPE;
   return check_rows(static_cast<long long>(B) * H * W, C, dtype);
 }
 static int check_grid_view(const lbp_view& v, int C, int dtype) {
@@ -160,6 +166,9 @@ static int run_grid(const void* g_y, const void* z, void* g_z, int B, int H, int
 static GradOf grad_of(const void* z, int H, int W, int C, const lbp_epilogue& e) {
   return GradOf{e.act != LBP_ACT_NONE ? z : nullptr, e.act, e.first, resolve_view(&e.number, H, W, C), drop_of(e)};
 }
+
+// Whether g_z is g_y.
+static bool does_nothing(const lbp_epilogue& e) { return e.act == LBP_ACT_NONE && !drop_of(e).on && e.used == nullptr; }
 
 static size_t grid_bytes(long long tokens, int C, int dtype) {
   return align_up(static_cast<size_t>(tokens) * C * elem_size(dtype), 1024);
@@ -297,7 +306,7 @@ int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, 
   if (int s = check_device_arch()) return s;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const GradOf of = grad_of(z, H, W, C, e);
-  const bool as_it_is = e.act == LBP_ACT_NONE && !of.drop.on && e.used == nullptr;   // g_z is g_y
+  const bool as_it_is = does_nothing(e);
   if (as_it_is || project_forms_gradient(dtype, B, H, W, k, r)) {
     if (!as_it_is) set_projection_gradient(&of);
     const int s = launch_project(g_y, t_hat, dtype, B, H, W, C, plan, static_cast<uint32_t*>(ws), st, 0.f, view);
@@ -312,7 +321,7 @@ int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, 
 size_t lbp_workspace_bytes_act(const lbp_layer* layer, int r, const lbp_extras* ex, int x_hat) {
   const lbp_extras d = with_dense_gradient(ex);
   const size_t inner = inner_bytes(layer, r, ex, x_hat != 0);
-  if (inner == 0) return 0;
+  if (inner == 0 || !fits_grid(layer->H, layer->W)) return 0;
   return inner + grid_bytes(d.n_extra, layer->Cout, layer->dtype) +
          (may_form(*layer, r, x_hat != 0) && d.g_bias == nullptr
               ? 0
@@ -338,8 +347,10 @@ int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const vo
   // the call as it is, for what is wrong with it apart from the epilogue
   if (int s = backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, true)) return s;
   const size_t need = lbp_workspace_bytes_act(layer, r, ex, x_hat != nullptr);
+  if (!fits_grid(layer->H, layer->W)) return LBP_ERR_SHAPE;
   if (need == 0 || ws_bytes < need) return LBP_ERR_WORKSPACE;
   if (int s = check_device_arch()) return s;
+  if (does_nothing(e)) return backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, false);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   lbp_extras d = with_dense_gradient(ex);
   const size_t inner = inner_bytes(layer, r, ex, x_hat != nullptr);

@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int col = at.n * p.BN + c * 64;
         const int cols = p.Cout - col;                           // of this chunk on
         const int here = row < p.rows ? cols : 0;                // ... in this thread's row
-        const uint32_t two_biases = p.bias != nullptr && 2 * lane < cols ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
+        const uint32_t two_biases = p.bias != nullptr && 2 * lane < cols ? *(reinterpret_cast<const uint32_t*>(p.bias + col) + lane) : 0u;
         const __nv_bfloat16* const res = p.residual + row * p.pr + col;
         uint32_t r[8];
         if constexpr (RES) read16(res, r, here, p.wide);
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           if (left <= g * 8) break;
-          Vec<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(p.bias + col + g * 8)), b);
+          Vec<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(p.bias + col + g * 8), b);
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[g * 8 + j] += b[j];
         }

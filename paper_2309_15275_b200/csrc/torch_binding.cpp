@@ -986,7 +986,8 @@ struct LayerFunction : public torch::autograd::Function<LayerFunction> {
       const int64_t B = x.size(0);
       n = x.size(1) - H * W;
       g_x = at::empty_like(x);
-      if (n > 1) {   // numbers of the extra tokens are no arithmetic series: the whole sequence at once
+      const bool changed = g.epilogue.act != LBP_ACT_NONE || g.epilogue.p > 0.f;
+      if (n > 1 && changed) {   // numbers of the extra tokens are no arithmetic series: the whole sequence at once
         Tensor g_z;
         const int s = run_pointwise(g_y, z, &g_z, g.epilogue, true);
         TORCH_CHECK_VALUE(s >= 0, "LbpLinear: gradient and kept activation do not fit together");

@@ -662,3 +662,41 @@ def test_dropout_repeats_under_checkpointing(dev):
         y = run()
         grads.append(torch.autograd.grad(y.square().sum(), (x, layer.weight)))
     assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_without_activation_and_dropout_it_is_the_plain_call(dev, dtype):
+    """The same launches, so the same bits; of a module too, with any number of class tokens."""
+    x, g = _normal((4, 16, 16, 192), 1.0, dtype, 0), _normal((4, 16, 16, 256), 0.1, dtype, 1)
+    w, bases = _normal((256, 192), 0.07, dtype, 2), O.select_bases(8, O.RULE_PREFIX, 8)
+    gb, gb2 = (torch.empty(256, device=dev) for _ in range(2))
+    gx, gw = lbp.lbp_backward_act(x, g, None, w, 8, bases, p=2.0 ** -18, g_bias=gb)
+    n = lbp.lbp_launch_count()
+    rx, rw = lbp.lbp_backward_ex(x, g, w, 8, bases, g_bias=gb2)
+    plain = lbp.lbp_launch_count() - n
+    n = lbp.lbp_launch_count()
+    lbp.lbp_backward_act(x, g, None, w, 8, bases, p=0.0, g_bias=gb)
+    assert lbp.lbp_launch_count() - n == plain
+    assert torch.equal(gx, rx) and torch.equal(gw, rw) and torch.equal(gb, gb2)
+    for cls in (0, 1, 2):
+        layer = lbp.LbpLinear(192, 256, 8, bases, bias=True, device=dev, dtype=dtype, grid=(16, 16))
+        s = _normal((4, cls + 256, 192), 1.0, dtype, 3).requires_grad_()
+        r = _normal((4, cls + 256, 256), 1.0, dtype, 4).requires_grad_()
+        gy = _normal((4, cls + 256, 256), 0.1, dtype, 5)
+        got = torch.autograd.grad(layer(s, residual=r), (s, r, layer.weight, layer.bias), gy)
+        want = torch.autograd.grad(layer(s), (s, layer.weight, layer.bias), gy)
+        assert torch.equal(got[1], gy)
+        assert all(torch.equal(a, b) for a, b in zip((got[0],) + got[2:], want))
+
+
+def test_expanded_operands_of_the_backward_pass_are_refused(dev):
+    """Their strides of zero would read as those of a dense tensor."""
+    w, bases = _normal((64, 64), 0.1, torch.bfloat16, 0), O.select_bases(8, O.RULE_PREFIX, 8)
+    one, full = _normal((1, 1, 1, 64), 1.0, torch.bfloat16, 1), _normal((2, 8, 8, 64), 1.0, torch.bfloat16, 2)
+    for x, g in ((one.expand(2, 8, 8, 64), full), (full, one.expand(2, 8, 8, 64))):
+        with pytest.raises(ValueError):
+            lbp.lbp_backward_ex(x, g, w, 8, bases)
+        with pytest.raises(ValueError):
+            lbp.lbp_backward_act(x, g, full, w, 8, bases, activation="gelu")
+    with pytest.raises(ValueError):
+        lbp.lbp_project_grad(one.expand(2, 8, 8, 64), full, 8, bases, activation="gelu")

@@ -231,3 +231,20 @@ def test_binding_refuses_on_the_cpu_and_names_the_error():
     layer = lbp.LbpLinear(64, 32, 8, [(0, 0)], activation="gelu")
     with pytest.raises(ValueError, match="CUDA"):
         layer(torch.zeros(1, 8, 8, 64))
+
+
+@pytest.mark.parametrize("more", [dict(seed_dev=8 * P, offset_dev=8 * P + 8, used=8 * P), dict(seed_dev=8 * P + 8, used=8 * P),
+                                  dict(offset_dev=8 * P, used=8 * P)])
+def test_used_may_not_be_what_is_read(more):
+    ep = _ep(p=0.5, **more)
+    assert _linear(ep=ep) == _pointwise("lbp_dropout", ep=ep) == _project(ep=ep) == _backward(ep=ep) == OVERLAP
+
+
+def test_sizes_past_the_kernels_integers_are_refused():
+    wide = (1 << 30) + 8
+    assert _linear(Cin=wide) == _linear(Cout=wide) == _pointwise("lbp_dropout", Cc=wide) == SHAPE
+    assert B._lib().lbp_linear_workspace_bytes(4, wide, 8, lbp.LBP_BF16) == 0
+    assert _project(B_=1, H=1 << 16, W=1 << 15, Cc=8) == SHAPE
+    lay = B._layer(1, 1 << 16, 1 << 15, 8, 8, 8, lbp.LBP_BF16, lbp.LBP_F32)
+    assert B._lib().lbp_workspace_bytes_act(C.byref(lay), 4, None, 0) == 0
+    assert _backward(lay=lay, n=1 << 50) == SHAPE
