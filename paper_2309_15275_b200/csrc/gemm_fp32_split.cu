@@ -193,7 +193,7 @@ __device__ __forceinline__ layer::Stream stream_of(const layer::LinearCall& p) {
   return p.drop.on ? layer::open_stream(p.drop) : layer::Stream{};
 }
 
-// The item of this CTA.  LIN: L is stored by lanes, in shared memory as two boxes of 32 k's in the 128-byte swizzle.
+// An item.  LIN: L is stored by lanes, in shared memory as two boxes of 32 k's in the 128-byte swizzle.
 template <int BN, bool LIN>
 struct Item {
   const CUtensorMap *map_l, *map_c;
@@ -206,20 +206,22 @@ struct Item {
   bool wt;               // L = B, C = A stored (columns, K), D transposed
   bool planes;           // K is shared with other items
 
-  __device__ __forceinline__ Item(const GemmFp32Jobs& jobs, const Maps& maps) {
+  __device__ __forceinline__ Item(const GemmFp32Jobs& jobs, const Maps& maps, int t) {
     extern __shared__ uint8_t smem_raw[];
     smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     raw = smem + 2 * Cfg<BN>::kStage;
     full = reinterpret_cast<uint64_t*>(raw + 2 * Cfg<BN>::kRaw);
     status = jobs.status;
-    int t = blockIdx.x;
     const int which = t >= jobs.items0 ? 1 : 0;
     const GemmFp32Job& g = jobs.j[which];
     map_l = &maps.l[which];
     map_c = &maps.c[which];
     if (which) t -= jobs.items0;
-    const int chunk = t % g.chunks;
-    t /= g.chunks;
+    int chunk = 0;
+    if (!LIN || g.chunks > 1) {   // (LIN: seldom, and a division of integers takes 0.1 us)
+      chunk = t % g.chunks;
+      t /= g.chunks;
+    }
     wt = !LIN && g.a_mn == 0;
     planes = g.chunks > 1;
     lanes = wt ? g.N : g.M;
@@ -232,11 +234,11 @@ struct Item {
     D = g.D + chunk * g.M * g.N;
   }
 
-  // One thread: the u-th load of this CTA, block u of the item (and u - n_kb once more from there on).
-  __device__ __forceinline__ void load(int u) const {
+  // One thread: the u-th load of this CTA, block i of the item.
+  __device__ __forceinline__ void load(int u, int i) const {
     using C = Cfg<BN>;
     uint8_t* const dst = raw + (u & 1) * C::kRaw;
-    const int k = (kb0 + (u < n_kb ? u : u - n_kb)) * kBK;
+    const int k = (kb0 + i) * kBK;
     ptx::mbar_expect_tx(&full[u & 1], C::kRaw);   // boxes count in full, also where they hang over an edge (zeros)
     if constexpr (LIN) {
       ptx::tma_load_2d(dst, map_l, &full[u & 1], k, l0);
@@ -259,16 +261,17 @@ __device__ __forceinline__ bool stays(float v) {
 }
 
 // The rest of an item by FMAs, with all threads of the CTA: its sums term by term, one k after
-// the other.  few: its only block has been fetched.  Otherwise the item is fetched once more,
-// and of the sums in smem = [kCols][threads] those that do not stay are replaced, in warps with
-// `mine` set.  A thread has kCols / 4 lanes (in runs of four) by 4 columns, which reads less
-// than a lane by kCols.  Not inlined, and with nothing handed over: registers that the kernel
-// spills for this path cost every item of one block 0.5 us.
+// the other, after `loads` loads of the CTA.  few: its only block is among them.  Otherwise the item is fetched once
+// more, and of the sums in smem = [kCols][threads] those that do not stay are replaced, in warps with
+// `mine` set.  LIN: there are no sums in smem; `mine` has a bit for each of a warp's lanes whose sums it has kept back, and
+// those alone leave.  A thread has kCols / 4 lanes (in runs of four) by 4 columns, which reads less
+// than a lane by kCols.
 template <int BN, class Out>
-__device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps& maps, const Out& epi, bool few, bool mine) {
+__device__ __forceinline__ void sum_by_fma(const GemmFp32Jobs& jobs, const Maps& maps, const Out& epi, int t, int loads, bool few,
+                                           uint32_t mine) {
   using C = Cfg<BN>;
   constexpr bool LIN = kLinear<Out>;
-  const Item<BN, LIN> item(jobs, maps);
+  const Item<BN, LIN> item(jobs, maps, t);
   const float* const old = reinterpret_cast<const float*>(item.smem);
   constexpr int kRuns = C::kCols / 16, kAlong = 8 / kRuns;   // runs of a thread; threads along the lanes
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -278,9 +281,9 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
   float sum[C::kCols];
 #pragma unroll
   for (int j = 0; j < C::kCols; ++j) sum[j] = 0.f;
-  const int first = few ? 0 : item.n_kb;
+  const int first = few ? loads - 1 : loads;
   if (threadIdx.x == 0 && !few)
-    for (int i = 0; i < 2 && i < item.n_kb; ++i) item.load(first + i);
+    for (int i = 0; i < 2 && i < item.n_kb; ++i) item.load(first + i, i);
   for (int i = 0; i < item.n_kb; ++i) {
     const int u = first + i;
     if (!__syncthreads_and(item.arrived(u, 6u))) {
@@ -288,7 +291,7 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
       break;
     }
     const float* const at = reinterpret_cast<const float*>(item.raw + (u & 1) * C::kRaw);
-    if (mine) {
+    if (mine != 0 && warp < kWarps) {   // (the warp of its own would read behind C's columns)
 #pragma unroll 1
       for (int k = 0; k < (few ? 8 : kBK); k += 4) {   // (beyond K a block is zero)
         float c[4][4];   // [k][column]
@@ -331,10 +334,10 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
       }
     }
     __syncthreads();
-    if (threadIdx.x == 0 && i + 2 < item.n_kb) item.load(u + 2);
+    if (threadIdx.x == 0 && i + 2 < item.n_kb) item.load(u + 2, i + 2);
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (warp == kWarps) return;
+  if (warp == kWarps || (LIN && mine == 0)) return;
   const layer::Stream stream = stream_of(epi);
   const long long l = item.l0 + (warp & 3) * 32 + run, n = item.c0 + (warp >> 2) * C::kCols + four;
 #pragma unroll
@@ -345,7 +348,7 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v[i][j] = sum[h * 16 + 4 * i + j];
-        if (!few) {
+        if (!LIN && !few) {
           const float was = old[(four + j) * kWarps * 32 + warp * 32 + h * 4 * kAlong + run + i];
           if (stays(was)) v[i][j] = was;
         }
@@ -360,13 +363,13 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
                                  : i == 2 ? make_float4(v[2][0], v[2][1], v[2][2], v[2][3])
                                           : make_float4(v[3][0], v[3][1], v[3][2], v[3][3]);
           const long long row = l + h * 4 * kAlong + i;
-          if (row < item.lanes && n < item.cols) emit(epi, stream, row, n, four_of, four_of, 4);
+          if (row < item.lanes && n < item.cols && ((mine >> (run + h * 4 * kAlong + i)) & 1u) != 0) emit(epi, stream, row, n, four_of, four_of, 4);
         }
         continue;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (l + h * 4 * kAlong + i < item.lanes && n < item.cols)
+        if (l + h * 4 * kAlong + i < item.lanes && n < item.cols && ((mine >> (run + h * 4 * kAlong + i)) & 1u) != 0)
           *reinterpret_cast<float4*>(item.D + (l + h * 4 * kAlong + i) * item.cols + n) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
       continue;
     }
@@ -380,30 +383,45 @@ __device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps&
   }
 }
 
-template <int BN, class Out>
+// Whether a thread has a sum that does not stay.
+template <int COLS>
+__device__ __forceinline__ bool any_goes(const float (&sum)[COLS]) {
+  float most = 0.f;
+  uint32_t least = ~0u;
+#pragma unroll
+  for (int j = 0; j < COLS; j += 2) {
+    // (a NaN stays; zero becomes the largest)
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(sum[j]), "f"(sum[j + 1]));
+    least = __vimin3_u32(least, __float_as_uint(sum[j]) * 2u - 1u, __float_as_uint(sum[j + 1]) * 2u - 1u);
+  }
+  return !(most <= kMostSum) || least < __float_as_uint(kLeastSum) * 2u - 1u;
+}
+
+// The same of this CTA's item.  Not inlined, and with nothing handed over: registers that the kernel spills for this path
+// cost every item of one block 0.5 us.
+template <int BN>
+__device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps& maps, bool few, bool mine) {
+  const int t = blockIdx.x;
+  const int blocks = few ? 1 : Item<BN, false>(jobs, maps, t).n_kb;
+  sum_by_fma<BN>(jobs, maps, NoEpilogue{}, t, blocks, few, mine ? ~0u : 0u);
+}
+
+template <int BN>
 __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __grid_constant__ GemmFp32Jobs jobs,
-                                                                    const __grid_constant__ Maps maps,
-                                                                    const __grid_constant__ Out epi) {
+                                                                    const __grid_constant__ Maps maps) {
   using C = Cfg<BN>;
-  constexpr bool LIN = kLinear<Out>;
-  const Item<BN, LIN> item(jobs, maps);
+  const Item<BN, false> item(jobs, maps, blockIdx.x);
   uint8_t *const smem = item.smem, *const raw = item.raw;
   uint64_t* const full = item.full;
   uint64_t* ready = full + 2;                                        // [2]: a block's parts are written
   uint64_t* done = ready + 2;                                        // [2]: its MMAs have completed
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool wt = item.wt, ck = LIN || wt;
+  const bool wt = item.wt;
   const int n_kb = item.n_kb;
   const bool few = n_kb == 1 && item.K - static_cast<long long>(item.kb0) * kBK <= kFewTerms;
 
   if (threadIdx.x == 0) {
-    if constexpr (LIN) {
-      if (blockIdx.x == 0 && epi.drop.used != nullptr) {
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        layer::note_used(epi.drop);
-      }
-    }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&full[i], 1);
       ptx::mbar_init(&ready[i], kWarps);
@@ -424,17 +442,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
   asm volatile("griddepcontrol.wait;" ::: "memory");   // launched as the kernel ahead ends
 
   if (few) {
-    if (threadIdx.x == 0) item.load(0);
-    finish_by_fma<BN>(jobs, maps, epi, true, true);
+    if (threadIdx.x == 0) item.load(0, 0);
+    finish_by_fma<BN>(jobs, maps, true, true);
     return;
   }
   // L: a thread has its lane's k's of one half of the block.  C: pieces of four numbers, a
   // warp whole 128-byte lines; row `row` + q * rows of the block, in shared memory `hop` apart.
   const bool is_l = warp < 8;
   const int quarter = warp & 3, tid = threadIdx.x & 255;
-  const int c_row = ck ? tid >> 4 : tid / (BN / 4), c_pc = ck ? tid & 15 : tid % (BN / 4);
-  const int hop = (ck ? 16 : 256 / (BN / 4)) * 128;
-  const int to = (ck ? 0 : (c_pc >> 4) * kChunkBytes) + c_row * 128 + ((((c_pc & 15) >> 1) ^ (c_row & 7)) << 4) + (c_pc & 1) * 8;
+  const int c_row = wt ? tid >> 4 : tid / (BN / 4), c_pc = wt ? tid & 15 : tid % (BN / 4);
+  const int hop = (wt ? 16 : 256 / (BN / 4)) * 128;
+  const int to = (wt ? 0 : (c_pc >> 4) * kChunkBytes) + c_row * 128 + ((((c_pc & 15) >> 1) ^ (c_row & 7)) << 4) + (c_pc & 1) * 8;
 
   float sum[C::kCols];
 #pragma unroll
@@ -460,14 +478,14 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
   int begun = 0;   // blocks whose MMAs this thread has issued
   if (warp == kWarps) {
     if (ptx::elect_one()) {
-      const uint32_t idesc = ptx::idesc_bf16(kLanes, BN, false, !ck);
+      const uint32_t idesc = ptx::idesc_bf16(kLanes, BN, false, !wt);
       const int n = jobs.test_stall ? 0 : n_kb;
       int loads = 0;   // blocks fetched
-      for (; loads < 2 && loads < n; ++loads) item.load(loads);
+      for (; loads < 2 && loads < n; ++loads) item.load(loads, loads);
       for (int i = 0; i < n_kb; ++i) {
         const int s = i & 1;
         if (!ptx::mbar_wait(&ready[s], static_cast<uint32_t>(i >> 1) & 1u, jobs.status, (7u << 16) | 3u)) break;
-        if (i + 2 < n_kb) item.load(loads++);   // everyone has read block i
+        if (i + 2 < n_kb) item.load(loads, loads), ++loads;   // everyone has read block i
         ptx::tc_fence_after_sync();
         const uint32_t a = tmem_base + kTmemL + s * 3 * kPartCols, b = ptx::smem_u32(smem + s * C::kStage);
         const uint32_t d = tmem_base + s * BN;
@@ -479,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 #pragma unroll
           for (int kk = 0; kk < kBK / 16; ++kk) {
             const uint32_t bp = b + kPc[q] * C::kPart;
-            const uint64_t db = ck ? ptx::smem_desc_sw128(bp + kk * 32, 16, 1024)
+            const uint64_t db = wt ? ptx::smem_desc_sw128(bp + kk * 32, 16, 1024)
                                    : ptx::smem_desc_sw128(bp + kk * 2048, kChunkBytes, 1024);
             const uint32_t al = a + kPl[q] * kPartCols + kk * 8;
             if (kk == 0 && (q == 1 || q == 5))
@@ -507,18 +525,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 #pragma unroll
       for (int h = 0; h < 2; ++h) {   // 16 k's
         float v[16];
-        if constexpr (LIN) {
-          const int l = quarter * 32 + lane;
-          const float* const row = reinterpret_cast<const float*>(raw + s * C::kRaw) + (warp >> 2) * (C::kRawL / 8) + l * 32;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float4 f = *reinterpret_cast<const float4*>(row + (((4 * h + j) ^ (l & 7)) << 2));
-            v[4 * j] = f.x, v[4 * j + 1] = f.y, v[4 * j + 2] = f.z, v[4 * j + 3] = f.w;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] = src[(16 * h + j) * kLanes];
-        }
+        for (int j = 0; j < 16; ++j) v[j] = src[(16 * h + j) * kLanes];
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
           uint32_t w[8];
@@ -569,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
 #pragma unroll
         for (int j = 0; j < C::kCols; ++j) reinterpret_cast<float*>(smem)[j * kWarps * 32 + threadIdx.x] = sum[j];
       }
-      finish_by_fma<BN>(jobs, maps, epi, false, __any_sync(0xffffffffu, bad));
+      finish_by_fma<BN>(jobs, maps, false, __any_sync(0xffffffffu, bad));
       return;
     }
     if (begun > 0)
@@ -595,21 +603,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
           make_float4(sum[4 * c], sum[4 * c + 1], sum[4 * c + 2], sum[4 * c + 3]);
     __syncwarp();
     const int c = lane % kRowPieces;
-    if constexpr (LIN) {
-      if (!item.planes) {
-        const layer::Stream stream = stream_of(epi);
-        constexpr int kEights = kRowPieces / 2;
-        const int e = lane % kEights;
-#pragma unroll 1
-        for (int row = lane / kEights; row < 32; row += 32 / kEights) {
-          const long long gm = item.l0 + quarter * 32 + row, gn = n0 + 8 * e;
-          const float4* const from = mine + row * kRowPieces;
-          const int flip = row & (kRowPieces - 1);
-          if (gm < lanes && gn < cols) emit(epi, stream, gm, gn, from[(2 * e) ^ flip], from[(2 * e + 1) ^ flip], cols - gn < 8 ? 4 : 8);
-        }
-        return;
-      }
-    }
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += 32 / kRowPieces) {
       const int row = r0 + lane / kRowPieces;
@@ -620,28 +613,310 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp32_split_kernel(const __gr
   }
 }
 
+// lbp_linear: a CTA has up to kMostItems items, gridDim apart.  Behind an item's last block the parts of the next item's
+// first two are written before its sums leave, so that their products run meanwhile.  Shared memory is full of the next
+// item then, so the lanes that share a stretch of channels exchange rows by shuffles and write 32 bytes of a row each,
+// whole lines together (a row a lane, which needs no exchange, costs 1 us an item in the L1's tags).
+// An item to a CTA, its sums through shared memory, against this: 3136 tokens 448 -> 1792 with GELU and dropout (350
+// items) 54.4 and 50.0 us, 50176 tokens 48 -> 192 57.1 and 35.8, 3136 tokens 1792 -> 448 (100 items) 46.6 and 46.4, 640
+// tokens 448 -> 1792 (140 items) 13.0 and 13.6.
+constexpr int kMostItems = 32;
+
+// Item q of this CTA; the blocks of an item.
+__device__ __forceinline__ int item_of(int q) { return static_cast<int>(blockIdx.x + q * gridDim.x); }
+__device__ __forceinline__ int items_here(const GemmFp32Jobs& jobs) {
+  const int grid = static_cast<int>(gridDim.x);
+  return jobs.items <= grid ? 1 : (jobs.items - static_cast<int>(blockIdx.x) + grid - 1) / grid;
+}
+__device__ __forceinline__ int blocks_of(const GemmFp32Jobs& jobs, int t) {
+  const GemmFp32Job& g = jobs.j[0];
+  if (g.chunks == 1) return g.kb;
+  const int from = t % g.chunks * g.per;
+  return (from + g.per < g.kb ? from + g.per : g.kb) - from;
+}
+
+// The items of this CTA that threads have kept back (a bit each), or with few terms all.
+template <int BN>
+__device__ __noinline__ void finish_by_fma(const GemmFp32Jobs& jobs, const Maps& maps, const layer::LinearCall& epi, bool few,
+                                           uint32_t kept_back) {
+  const int n_items = items_here(jobs);
+  int loads = 0;
+  for (int q = 0; q < n_items && !few; ++q) loads += blocks_of(jobs, item_of(q));
+  for (int q = 0; q < n_items; ++q) {
+    const uint32_t mine = few ? ~0u : __ballot_sync(0xffffffffu, ((kept_back >> q) & 1u) != 0);
+    if (!__syncthreads_or(mine != 0)) continue;
+    const int t = item_of(q);
+    if (few && threadIdx.x == 0) Item<BN, true>(jobs, maps, t).load(q, 0);
+    if (few) ++loads;
+    sum_by_fma<BN>(jobs, maps, epi, t, loads, few, mine);
+    if (!few) loads += blocks_of(jobs, t);
+  }
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kThreads, 1) linear_fp32_kernel(const __grid_constant__ GemmFp32Jobs jobs,
+                                                                const __grid_constant__ Maps maps,
+                                                                const __grid_constant__ layer::LinearCall epi) {
+  using C = Cfg<BN>;
+  using It = Item<BN, true>;
+  const It first(jobs, maps, blockIdx.x);
+  uint8_t *const smem = first.smem, *const raw = first.raw;
+  uint64_t* const full = first.full;
+  uint64_t* const ready = full + 2;                                        // [2]: a block's parts are written
+  uint64_t* const done = ready + 2;                                        // [2]: its MMAs have completed
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_items = items_here(jobs);
+  const bool few = first.K <= kFewTerms;
+
+  if (threadIdx.x == 0) {
+    if (blockIdx.x == 0 && epi.drop.used != nullptr) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      layer::note_used(epi.drop);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&full[i], 1);
+      ptx::mbar_init(&ready[i], kWarps);
+      ptx::mbar_init(&done[i], 1);
+    }
+    ptx::mbar_fence_init();
+    ptx::prefetch_tensormap(first.map_l);
+    ptx::prefetch_tensormap(first.map_c);
+  }
+  if (warp == 0 && !few) {
+    ptx::tmem_alloc(tmem_slot, kTmemCols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;   // (few: none)
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // launched as the kernel ahead ends
+
+  if (few) {
+    finish_by_fma<BN>(jobs, maps, epi, true, 0u);
+    return;
+  }
+  // L: a thread has its lane's k's of one half of the block.  C: pieces of four numbers, a warp whole 128-byte lines;
+  // row `row` + q * 16 of the block, in shared memory `hop` apart.
+  const bool is_l = warp < 8;
+  const int quarter = warp & 3, group = warp >> 2, tid = threadIdx.x & 255;
+  const int c_row = tid >> 4, c_pc = tid & 15;
+  constexpr int hop = 16 * 128;
+  const int to = c_row * 128 + (((c_pc >> 1) ^ (c_row & 7)) << 4) + (c_pc & 1) * 8;
+  const uint32_t lane_bits = static_cast<uint32_t>(quarter * 32) << 16;
+  const uint32_t acc_at = tmem_base + lane_bits + group * C::kCols;
+  float sum[C::kCols];
+#pragma unroll
+  for (int j = 0; j < C::kCols; ++j) sum[j] = 0.f;
+  bool ok = true;
+  uint32_t bad_items = 0;   // those whose sums this thread has kept back
+  auto split = [&](int u) {
+    const int s = u & 1;
+    ok = __all_sync(0xffffffffu, first.arrived(u, 2u));
+    if (!ok) return;
+    // (the MMAs that read this stage of parts have completed: their accumulator was drained)
+    if (is_l) {
+      const float* const row = reinterpret_cast<const float*>(raw + s * C::kRaw) + (warp >> 2) * (C::kRawL / 8) + (quarter * 32 + lane) * 32;
+      const uint32_t dst = tmem_base + lane_bits + kTmemL + s * 3 * kPartCols + (warp >> 2) * 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {   // 16 k's
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 f = *reinterpret_cast<const float4*>(row + (((4 * h + j) ^ (lane & 7)) << 2));
+          v[4 * j] = f.x, v[4 * j + 1] = f.y, v[4 * j + 2] = f.z, v[4 * j + 3] = f.w;
+        }
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          uint32_t w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = take_part(v[2 * j], v[2 * j + 1], part);
+          tmem_st_x8(dst + part * kPartCols + h * 8, w);
+        }
+      }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+    } else {
+      const float4* const src = reinterpret_cast<const float4*>(raw + s * C::kRaw + C::kRawL) + tid;
+      uint8_t* const dst = smem + s * C::kStage + to;
+#pragma unroll
+      for (int q = 0; q < C::kPieces; ++q) {
+        float4 v = src[q * 256];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const uint32_t w0 = take_part(v.x, v.y, part), w1 = take_part(v.z, v.w, part);
+          *reinterpret_cast<uint2*>(dst + q * hop + part * C::kPart) = make_uint2(w0, w1);
+        }
+      }
+      ptx::fence_proxy_async_smem();   // the tensor core reads the parts through the async proxy
+    }
+    ptx::tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&ready[s]);
+  };
+  auto drain = [&](int u) {
+    ok = __all_sync(0xffffffffu,
+                    ptx::mbar_wait(&done[u & 1], static_cast<uint32_t>(u >> 1) & 1u, jobs.status, (7u << 16) | 1u));
+    ptx::tc_fence_after_sync();
+#pragma unroll
+    for (int c = 0; c < C::kCols; c += 16) {
+      uint32_t a[16];
+      ptx::tmem_ld_xn<16>(acc_at + (u & 1) * BN + c, a);
+      ptx::tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sum[c + j] += __uint_as_float(a[j]);
+    }
+  };
+  int32_t l0 = first.l0, c0 = first.c0;   // of the item that is being summed
+  float* plane = first.D;
+  auto finish = [&](int q) {
+    constexpr int kPieces = C::kCols / 8;   // of eight channels
+    const bool goes = any_goes(sum);
+    if (goes) bad_items |= 1u << q;
+    const uint32_t bad_rows = __ballot_sync(0xffffffffu, goes);
+    // kPieces lanes exchange theirs: lane j of them gets channels 8 j on of all their rows
+#pragma unroll
+    for (int d = 1; d < kPieces; d *= 2) {
+      const bool up = (lane & d) != 0;
+#pragma unroll
+      for (int j = 0; j < C::kCols; ++j) {
+        if ((j >> 3) & d) continue;
+        const float got = __shfl_xor_sync(0xffffffffu, up ? sum[j] : sum[j + 8 * d], d);
+        sum[j] = up ? got : sum[j];
+        sum[j + 8 * d] = up ? sum[j + 8 * d] : got;
+      }
+    }
+    const layer::Stream stream = stream_of(epi);
+    const int row0 = lane & ~(kPieces - 1);   // of this warp's
+    const long long ch = c0 + group * C::kCols + (lane & (kPieces - 1)) * 8;
+#pragma unroll 1
+    for (int i = 0; i < kPieces; ++i) {
+      const long long row = l0 + quarter * 32 + row0 + i;
+      const float4 lo = make_float4(sum[0], sum[1], sum[2], sum[3]), hi = make_float4(sum[4], sum[5], sum[6], sum[7]);
+      if (row < first.lanes && ch < first.cols && ((bad_rows >> (row0 + i)) & 1u) == 0) {
+        if (first.planes) {
+          float4* const to = reinterpret_cast<float4*>(plane + row * first.cols + ch);
+          to[0] = lo;
+          if (ch + 4 < first.cols) to[1] = hi;
+        } else {
+          emit(epi, stream, row, ch, lo, hi, first.cols - ch < 8 ? 4 : 8);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j + 8 < C::kCols; ++j) sum[j] = sum[j + 8];
+    }
+#pragma unroll
+    for (int j = 0; j < C::kCols; ++j) sum[j] = 0.f;
+  };
+
+  int begun = 0;   // blocks whose MMAs this thread has issued
+  if (warp == kWarps) {
+    if (ptx::elect_one()) {
+      const uint32_t idesc = ptx::idesc_bf16(kLanes, BN, false, false);
+      It at = first;                                     // of the next load
+      int loads = 0, q_at = jobs.test_stall ? n_items : 0, i_at = 0;
+      auto load = [&] {
+        if (q_at >= n_items) return;
+        at.load(loads++, i_at);
+        if (++i_at < at.n_kb) return;
+        i_at = 0;
+        if (++q_at < n_items) at = It(jobs, maps, item_of(q_at));
+      };
+      load();
+      load();
+      for (int q = 0; q < n_items && ok; ++q)
+        for (int i = blocks_of(jobs, item_of(q)); i > 0 && ok; --i) {
+          const int s = begun & 1;
+          ok = ptx::mbar_wait(&ready[s], static_cast<uint32_t>(begun >> 1) & 1u, jobs.status, (7u << 16) | 3u);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const uint32_t a = tmem_base + kTmemL + s * 3 * kPartCols, b = ptx::smem_u32(smem + s * C::kStage);
+          const uint32_t d = tmem_base + s * BN;
+          constexpr int kPl[6] = {1, 2, 0, 1, 0, 0}, kPc[6] = {1, 0, 2, 0, 1, 0};   // (as above)
+#pragma unroll
+          for (int w = 0; w < 6; ++w)
+#pragma unroll
+            for (int kk = 0; kk < kBK / 16; ++kk) {
+              const uint64_t db = ptx::smem_desc_sw128(b + kPc[w] * C::kPart + kk * 32, 16, 1024);
+              const uint32_t al = a + kPl[w] * kPartCols + kk * 8;
+              if (kk == 0 && (w == 1 || w == 5))
+                mma_bf16_ts_down(d, al, db, idesc);
+              else
+                mma_bf16_ts(d, al, db, idesc, (w == 0 && kk == 0) ? 0u : 1u);
+            }
+          ptx::mma_commit(&done[s]);
+          ++begun;
+          load();   // everyone has read the block of this stage
+        }
+      // (after an expired wait: no load is under way when the CTA ends)
+      for (int u = begun; u < loads; ++u) first.arrived(u, 4u);
+    }
+    __syncwarp();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (counts when all threads have)
+  } else {
+    int total = n_items * jobs.j[0].kb;
+    if (jobs.j[0].chunks > 1) {
+      total = 0;
+      for (int q = 0; q < n_items; ++q) total += blocks_of(jobs, item_of(q));
+    }
+    int q = 0, left = blocks_of(jobs, item_of(0));   // the item that is being summed, its blocks to come
+    bool summed = false;                             // the item before it has not been sent yet
+#pragma unroll 1
+    for (int u = 0; u < total + 2 && ok; ++u) {
+      if (u < total) split(u);
+      if (!ok) break;
+      if (summed) {   // under the products of the next item's first two blocks
+        finish(q - 1);
+        if (q < n_items) {
+          const It item(jobs, maps, item_of(q));
+          l0 = item.l0, c0 = item.c0, plane = item.D;
+        }
+      }
+      summed = false;
+      if (u == 0 || u > total) continue;
+      drain(u - 1);                // under the MMAs just issued
+      if (--left > 0) continue;
+      summed = true;
+      if (++q < n_items) left = blocks_of(jobs, item_of(q));
+      // The next kernel may start, as late as this: CTAs that come early, while some SMs are
+      // idle, would all settle on those.
+      else asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
+  }
+  ptx::tc_fence_before_sync();
+  // past this barrier every load, MMA and read of TMEM and shared memory has ended, unless a wait ran out
+  const bool expired = __syncthreads_or(!ok);
+  if (expired) {
+    if (begun > 0)
+      ptx::mbar_wait(&done[(begun - 1) & 1], static_cast<uint32_t>((begun - 1) >> 1) & 1u, jobs.status, (7u << 16) | 5u);
+    __syncthreads();
+  }
+  if (warp == 0) ptx::tmem_dealloc(tmem_base, kTmemCols);
+  if (!__syncthreads_or(bad_items != 0) || expired) return;
+  finish_by_fma<BN>(jobs, maps, epi, false, bad_items);
+}
+
 }  // namespace split
 
 static thread_local bool g_test_stall = false;
 void set_test_stall_fp32(bool on) { g_test_stall = on; }
 
-template <int BN, class Out>
-static int launch_items(const GemmFp32Jobs& js, const split::Maps& maps, const Out& out, cudaStream_t stream) {
+template <int BN, class Kernel, class... Out>
+static int launch_items(Kernel kern, PerDevice& configured, int ctas, const GemmFp32Jobs& js, const split::Maps& maps,
+                        cudaStream_t stream, const Out&... out) {
   using C = split::Cfg<BN>;
-  static PerDevice configured;
-  const auto kern = split::gemm_fp32_split_kernel<BN, Out>;
   if (int e = allow_dynamic_smem(configured, reinterpret_cast<const void*>(kern), C::kSmem)) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(js.items);
+  cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(split::kThreads);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = stream;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, js, maps, out));
+  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, js, maps, out...));
   count_launch();
   return LBP_OK;
 }
@@ -659,7 +934,8 @@ static int launch_bn(const GemmFp32Jobs& js, int n, cudaStream_t stream) {
       if (int e = encode_f32_matrix_map(&maps.c[i], g.A, g.M, g.K, BN, split::kBK)) return e;
     }
   }
-  return launch_items<BN>(js, maps, split::NoEpilogue{}, stream);
+  static PerDevice configured;
+  return launch_items<BN>(split::gemm_fp32_split_kernel<BN>, configured, js.items, js, maps, stream);
 }
 
 int launch_gemm_fp32_split(GemmFp32Jobs& js, int n, int bn, cudaStream_t stream) {
@@ -741,7 +1017,15 @@ int launch_linear_fp32(const LinearCall& c, cudaStream_t stream) {
   if (int e = encode_f32_matrix_map(&maps.c[0], c.W, c.Cout, c.Cin, how.bn, split::kBK)) return e;
   maps.l[1] = maps.l[0];
   maps.c[1] = maps.c[0];
-  if (int e = how.bn == 64 ? launch_items<64>(js, maps, c, stream) : launch_items<128>(js, maps, c, stream)) return e;
+  int dev = 0, sms = 0;
+  LBP_CUDA_TRY(cudaGetDevice(&dev));
+  LBP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int least = (js.items + split::kMostItems - 1) / split::kMostItems, at_once = js.items < sms ? js.items : sms;
+  const int ctas = least > at_once ? least : at_once;
+  static PerDevice configured[2];
+  if (int e = how.bn == 64 ? launch_items<64>(split::linear_fp32_kernel<64>, configured[0], ctas, js, maps, stream, c)
+                           : launch_items<128>(split::linear_fp32_kernel<128>, configured[1], ctas, js, maps, stream, c))
+    return e;
   if (how.chunks == 1) return LBP_OK;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr;

@@ -700,3 +700,49 @@ def test_expanded_operands_of_the_backward_pass_are_refused(dev):
             lbp.lbp_backward_act(x, g, full, w, 8, bases, activation="gelu")
     with pytest.raises(ValueError):
         lbp.lbp_project_grad(one.expand(2, 8, 8, 64), full, 8, bases, activation="gelu")
+
+
+@pytest.mark.parametrize("rows,Cin,Cout", [
+    (620000, 8, 8),      # more tiles than the SMs take in 32 turns each, a block of K to a tile
+    (20000, 4, 4),       # few terms
+    (40000, 200, 72), (3300, 448, 1792), (9000, 64, 260),
+])
+def test_linear_fp32_of_many_tiles(dev, rows, Cin, Cout):
+    """A CTA has several tiles; y is the residual itself, and what is not finite stays in its rows."""
+    x, W, b = _inputs(rows, Cin, Cout, torch.float32, 4)
+    res = _normal((rows, Cout), 1.0, torch.float32, 6)
+    y, z = res.clone(), torch.empty_like(res)
+    lbp.lbp_linear(x, W, b, activation="gelu", residual=y, out=y, z=z, p=0.25, seed=5, offset=12)
+    bad = torch.tensor([0, rows // 3, rows // 3 + 1, rows // 2, rows - 1])
+    pick = torch.unique(torch.cat([bad + 2, torch.arange(130), torch.randint(0, rows, (300,), generator=torch.Generator().manual_seed(2)),
+                                   torch.arange(rows - 130, rows)]).clamp(max=rows - 1)).cuda()
+    zw = x[pick].double() @ W.double().t() + b.double()
+    dz = Cin * 2.0 ** -23 * f64(x[pick].double().abs() @ W.double().abs().t() + b.double().abs())
+    v = Y.act(f64(zw), "gelu")
+    d = Y.drop(v, f64(pick)[:, None].astype(np.int64) * Cout + np.arange(Cout)[None, :], 0.25, 5, 12)
+    r = f64(res[pick])
+    _check_linear(torch.float32, y[pick], z[pick], (f64(zw), d + r, dz, v, np.abs(r) + np.abs(d)), 0.25)
+    ref = x.double() @ W.double().t() + b.double()
+    S = x.double().abs() @ W.double().abs().t() + b.double().abs()
+    assert bool(((z.double() - ref).abs() <= 2.0 ** -24 * ref.abs() + Cin * 2.0 ** -23 * S).all())
+    # rows that are not finite, in several tiles
+    xb = x.clone()
+    xb[bad, 1] = float("nan")
+    xb[rows // 2, 1] = float("inf")
+    yb, zb = res.clone(), torch.empty_like(res)
+    lbp.lbp_linear(xb, W, b, activation="gelu", residual=yb, out=yb, z=zb, p=0.25, seed=5, offset=12)
+    others = torch.ones(rows, dtype=torch.bool, device=dev)
+    others[bad] = False
+    assert torch.equal(yb[others], y[others]) and torch.equal(zb[others], z[others])
+    assert not bool(torch.isfinite(zb[bad]).any())
+    numbers = np.asarray(bad, dtype=np.int64)[:, None] * Cout + np.arange(Cout)[None, :]
+    kept = torch.from_numpy(Y.keep(numbers, 0.25, 5, 12)).to(dev)
+    assert torch.equal(yb[bad][~kept], res[bad][~kept])
+    # a column of W that is not finite: its channel alone
+    Wb = W.clone()
+    Wb[3, 0] = float("nan")
+    zc = torch.empty_like(res)
+    lbp.lbp_linear(x, Wb, b, z=zc, save_z=True)
+    assert bool(torch.isnan(zc[:, 3]).all())
+    keep = [c for c in range(Cout) if c != 3]
+    assert bool(((zc.double() - ref).abs() <= 2.0 ** -24 * ref.abs() + Cin * 2.0 ** -23 * S)[:, keep].all())
