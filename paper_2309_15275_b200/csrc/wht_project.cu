@@ -76,6 +76,8 @@ __global__ void __launch_bounds__(ProjCfg<K, sizeof(T) == 2>::kWarps * 32, 1)
                      chunk * ch_per_tile, bw * K, bh * K, b);
   };
 
+  // nothing is read or written before the kernel ahead has completed
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (lane == 0) {
     for (uint32_t i = 0; i < S && i < n_my; ++i) issue(i, i);
   }
@@ -206,9 +208,18 @@ static int launch_one(const CUtensorMap* tmaps, T* out0, T* out1, const ProjPara
   if (int e = allow_dynamic_smem(configured, reinterpret_cast<const void*>(kern), Cfg::kSmemBytes)) return e;
   const uint32_t want = (p.n_items + Cfg::kWarps - 1) / Cfg::kWarps;
   const int grid = static_cast<int>(want < static_cast<uint32_t>(sms) ? want : sms);
-  kern<<<grid, Cfg::kWarps * 32, Cfg::kSmemBytes, stream>>>(tmaps[0], tmaps[1], out0, out1, p, plan);
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its start under the end of the kernel ahead
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(Cfg::kWarps * 32);
+  cfg.dynamicSmemBytes = Cfg::kSmemBytes;
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LBP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, tmaps[0], tmaps[1], out0, out1, p, plan));
   count_launch();
-  LBP_CUDA_TRY(cudaGetLastError());
   return LBP_OK;
 }
 
