@@ -49,7 +49,7 @@
 // and 1120); 2048 x 768 -> 3072: 115, 250 and 803 (436; 1690 and 6850).
 //
 // lbp_linear on fp32 data is a third use, with L = x and C = W, both stored by rows (K contiguous), so that a lane is
-// a token and the sums leave with the epilogue applied: `Out` is layer::LinearCall instead of NoEpilogue.
+// a token and the sums leave with the epilogue applied: linear_fp32_kernel, with `Out` layer::LinearCall instead of NoEpilogue.
 #include <type_traits>
 
 #include "gemm_fp32.cuh"
