@@ -873,6 +873,11 @@ def lbp_backward_act(x, g_y, z, W, k: int, bases, *, activation="none", p: float
     z_extra are laid out as g_y and gy_extra.  `first`, `number` (image, row, token), `first_extra` and
     `number_extra` number the elements for drop() as in the forward call (default: the dense grid
     alone); for the tokens of a (B, n + H*W, C) sequence first = n*C, number = ((n + H*W)*C, W*C, C)."""
+    got = _native().backward_act(x, x_hat, g_y, W, k, bases, float(beta), g_bias, x_extra, gy_extra, gx_extra, gw_dtype,
+                                 g_x, g_W, ws, z, activation, p, seed, offset, rng, z_extra, first, number, first_extra,
+                                 number_extra)
+    if got is not None:
+        return _result(got, "lbp_backward_act")
     if (x is None) == (x_hat is None):
         raise ValueError("give exactly one of x and x_hat")
     if g_y.dim() != 4:

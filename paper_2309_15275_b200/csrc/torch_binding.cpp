@@ -394,18 +394,22 @@ int run_ex(ExCall* c, const lbp_basis* set, int r) {
 }
 
 // backward_ex(x, x_hat, g_y, W, k, bases, beta, g_bias, x_extra, gy_extra, gx_extra, gw_dtype, g_x, g_W, ws)
+bool parse_ex(PyObject* const* a, ExCall* c, Bases* b) {
+  if (!parse_tensor(a[0], &c->x) || !parse_tensor(a[1], &c->x_hat) || !parse_tensor(a[2], &c->g_y) ||
+      !parse_tensor(a[3], &c->W) || !parse_int(a[4], &c->k) || !parse_bases(a[5], b) || !PyFloat_Check(a[6]) ||
+      !parse_tensor(a[7], &c->g_bias) || !parse_tensor(a[8], &c->x_extra) || !parse_tensor(a[9], &c->gy_extra) ||
+      !parse_tensor(a[10], &c->gx_extra) || !parse_tensor(a[12], &c->g_x) || !parse_tensor(a[13], &c->g_W) ||
+      !parse_tensor(a[14], &c->ws) || (c->g_bias.defined() && c->g_bias.scalar_type() != at::kFloat))
+    return false;
+  c->beta = PyFloat_AS_DOUBLE(a[6]);
+  c->gw_code = parse_dtype(a[11]);
+  return true;
+}
 PyObject* py_backward_ex(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   ExCall c;
   Bases b;
-  if (n != 15 || !parse_tensor(a[0], &c.x) || !parse_tensor(a[1], &c.x_hat) || !parse_tensor(a[2], &c.g_y) ||
-      !parse_tensor(a[3], &c.W) || !parse_int(a[4], &c.k) || !parse_bases(a[5], &b) || !PyFloat_Check(a[6]) ||
-      !parse_tensor(a[7], &c.g_bias) || !parse_tensor(a[8], &c.x_extra) || !parse_tensor(a[9], &c.gy_extra) ||
-      !parse_tensor(a[10], &c.gx_extra) || !parse_tensor(a[12], &c.g_x) || !parse_tensor(a[13], &c.g_W) ||
-      !parse_tensor(a[14], &c.ws) || (c.g_bias.defined() && c.g_bias.scalar_type() != at::kFloat))
-    return not_handled();
-  c.beta = PyFloat_AS_DOUBLE(a[6]);
-  c.gw_code = parse_dtype(a[11]);
+  if (n != 15 || !parse_ex(a, &c, &b)) return not_handled();
   const int e = without_gil([&] { return run_ex(&c, b.v, b.r); });
   if (e < 0) return not_handled();
   return e != LBP_OK ? PyLong_FromLong(e) : pair(c.g_x, c.g_W);
@@ -855,6 +859,57 @@ PyObject* py_project_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+bool parse_i64(PyObject* o, int64_t* v) {
+  if (!PyLong_Check(o)) return false;
+  *v = PyLong_AsLongLong(o);
+  if (PyErr_Occurred() == nullptr) return true;
+  PyErr_Clear();
+  return false;
+}
+
+// backward_act(the fifteen of backward_ex, z, activation, p, seed, offset, rng, z_extra, first, number, first_extra,
+//              number_extra)
+PyObject* py_backward_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  ExCall c;
+  Bases b;
+  Tensor z, z_extra, rng;
+  lbp_layer_grad g{};
+  lbp_epilogue& e = g.epilogue;
+  if (n != 26 || !parse_ex(a, &c, &b) || !parse_tensor(a[15], &z) || !parse_act(a[16], &e.act) ||
+      !parse_drop(a + 17, &e, &rng) || !parse_tensor(a[21], &z_extra) || !parse_i64(a[22], &e.first) ||
+      !parse_i64(a[24], &g.first_extra) || !parse_i64(a[25], &g.number_extra) || !on_current_device(c.g_y) ||
+      !use_rng(rng, c.g_y.get_device(), &e))
+    return not_handled();
+  if (a[23] != Py_None) {
+    if (!PyTuple_Check(a[23]) || PyTuple_GET_SIZE(a[23]) != 3 || !parse_i64(PyTuple_GET_ITEM(a[23], 0), &e.number.image) ||
+        !parse_i64(PyTuple_GET_ITEM(a[23], 1), &e.number.row) || !parse_i64(PyTuple_GET_ITEM(a[23], 2), &e.number.token))
+      return not_handled();
+  }
+  const int dev = c.g_y.get_device();
+  if (z.defined()) {
+    lbp_view v, vz;
+    if (z.scalar_type() != c.g_y.scalar_type() || z.sizes() != c.g_y.sizes() || !view_of(c.g_y, dev, &v) ||
+        !view_of(z, dev, &vz) || vz.image != v.image || vz.row != v.row || vz.token != v.token)
+      return not_handled();
+    g.z = z.data_ptr();
+  } else if (e.act != LBP_ACT_NONE) {
+    return not_handled();
+  }
+  if (z_extra.defined()) {
+    int64_t pitch, pz;
+    if (!c.gy_extra.defined() || z_extra.scalar_type() != c.g_y.scalar_type() || z_extra.sizes() != c.gy_extra.sizes() ||
+        z_extra.dim() != 2 || !rows_of(c.gy_extra, dev, &pitch) || !rows_of(z_extra, dev, &pz) || pz != pitch)
+      return not_handled();
+    g.z_extra = z_extra.data_ptr();
+  }
+  c.grad = &g;
+  const int s = without_gil([&] { return run_ex(&c, b.v, b.r); });
+  if (s < 0) return not_handled();
+  return s != LBP_OK ? PyLong_FromLong(s) : pair(c.g_x, c.g_W);
+  END_HANDLE_TH_ERRORS
+}
+
 // The state that one forward pass draws its numbers from: torch's generator of the device, so
 // that torch.manual_seed and a captured graph's replays have the meaning they have for torch's
 // own dropout.
@@ -1162,6 +1217,7 @@ PyMethodDef methods[] = {{"load", py_load, METH_VARARGS, nullptr},
                          LBP_FAST("linear_grad", py_linear_grad),
                          LBP_FAST("dropout", py_dropout),
                          LBP_FAST("project_grad", py_project_grad),
+                         LBP_FAST("backward_act", py_backward_act),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lbp_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

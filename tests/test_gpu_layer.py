@@ -746,3 +746,46 @@ def test_linear_fp32_of_many_tiles(dev, rows, Cin, Cout):
     assert bool(torch.isnan(zc[:, 3]).all())
     keep = [c for c in range(Cout) if c != 3]
     assert bool(((zc.double() - ref).abs() <= 2.0 ** -24 * ref.abs() + Cin * 2.0 ** -23 * S)[:, keep].all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_backward_act_of_a_sequence_by_either_way_into_the_library(dev, dtype, monkeypatch):
+    """The native binding and the one by ctypes: the same bits, and the same refusals."""
+    from paper_2309_15275_b200 import binding
+    B, H, Cin, Cout = 3, 8, 64, 96
+    bases = O.select_bases(8, O.RULE_PREFIX, 8)
+    seq = [_normal((B, 1 + H * H, c), 1.0, dtype, i) for i, c in enumerate((Cin, Cout, Cout))]
+    x, g, z = (t[:, 1:].unflatten(1, (H, H)) for t in seq)
+    w = _normal((Cout, Cin), 0.1, dtype, 5)
+
+    def call(**more):
+        gxe, gb = torch.empty(B, Cin, dtype=dtype, device=dev), torch.empty(Cout, device=dev)
+        kw = dict(activation="silu", p=0.3, seed=7, offset=4, g_bias=gb, x_extra=seq[0][:, 0], gy_extra=seq[1][:, 0],
+                  z_extra=seq[2][:, 0], gx_extra=gxe, first=Cout, number=((1 + H * H) * Cout, H * Cout, Cout),
+                  number_extra=(1 + H * H) * Cout)
+        gx, gw = lbp.lbp_backward_act(x, g, more.pop("z", z), w, 8, bases, **{**kw, **more})
+        return gx, gw, gb, gxe
+
+    bad = [dict(z=None), dict(z=z.contiguous()), dict(z_extra=seq[2][:, 0].contiguous()), dict(activation="tanh"), dict(p=1.5),
+           dict(seed=-1), dict(rng=torch.zeros(2, device=dev)), dict(first=-8), dict(number=(0, 0, -8))]
+    native = call()
+    gz = lbp.lbp_linear_grad(seq[1], seq[2], activation="silu", p=0.3, seed=7, offset=4)
+    gxe, gb = torch.empty(B, Cin, dtype=dtype, device=dev), torch.empty(Cout, device=dev)
+    gx, gw = lbp.lbp_backward_ex(x, gz[:, 1:].unflatten(1, (H, H)), w, 8, bases, g_bias=gb, x_extra=seq[0][:, 0], gy_extra=gz[:, 0],
+                                 gx_extra=gxe)
+    tol = 3 * 2.0 ** -9 if dtype == torch.bfloat16 else 1e-5
+    assert max(_rel(a, b) for a, b in zip(native, (gx, gw, gb, gxe))) <= tol
+    for kw in bad:
+        with pytest.raises((ValueError, RuntimeError)):
+            call(**kw)
+    module = binding._native()
+
+    class Without:
+        def __getattr__(self, name):
+            return (lambda *a: None) if name == "backward_act" else getattr(module, name)
+
+    monkeypatch.setattr(binding, "_native", lambda: Without())
+    assert all(torch.equal(a, b) for a, b in zip(native, call()))
+    for kw in bad:
+        with pytest.raises((ValueError, RuntimeError)):
+            call(**kw)
