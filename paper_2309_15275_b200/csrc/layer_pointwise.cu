@@ -36,7 +36,8 @@ template <class T, int ACT, bool DROP, bool FLAT, int U>
 __global__ void __launch_bounds__(256) pointwise_kernel(const __grid_constant__ PointCall p, const __grid_constant__ Grid grid) {
   using V = Vec<T>;
   const long long i0 = blockIdx.x * (256ll * U) + threadIdx.x;
-  // (the kernel ahead may still write what is read here)
+  // The kernel ahead may still write what is read here.  (The next one may start when this ends: let in earlier, its
+  // blocks take the places of this one's, 11.4 us become 11.9, with lbp_project behind it 16.4 become 17.1.)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const Stream s = DROP ? open_stream(p.drop) : Stream{};
   if (blockIdx.x == 0 && threadIdx.x == 0) note_used(p.drop);
