@@ -166,12 +166,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // 2 sqrt(2/pi) and 0.044715 times that: gelu_tanh(z) = z / (1 + exp(-(A z + B z^3)))
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.071354816272600247f;
 
-// The normal distribution's tail Phi(-a), a >= 0, as exp(-a^2/2) times a polynomial in t = 1 / (1 + c a), fitted
-// (weighted least squares towards the smallest largest error):
-//   exp(a^2/2) a Phi(-a) = S(t), c = 0.4, off by at most 8.6e-5 (S + 0.002).  With it gelu(z) =
-//       max(z, 0) - |z| Phi(-|z|) needs no case for infinities: t, exp(-a^2/2) and S stay finite.
-//   exp(a^2/2) Phi(-a) = Q(t), c = 0.38, off by at most 3.7e-5 Q; FINE: c = 0.275, 5.1e-8 Q, 3.9e-7 as evaluated.
-// a: not above 100.  Hands out exp(-a^2/2) and -Q.
+// The normal distribution's tail Phi(-a), a >= 0, as exp(-a^2/2) Q, with Q = exp(a^2/2) Phi(-a) a polynomial in t = 1 / (1 + c a),
+// fitted (weighted least squares towards the smallest largest error): c = 0.38, off by at most 3.7e-5 Q; FINE: c = 0.275,
+// 5.1e-8 Q, 3.9e-7 as evaluated.  gelu(z) = max(z, 0) - a Phi(-a), a = |z|.
+// a: not above 100 (exp(-a^2/2) is 0 there, and an infinity times that would be NaN).  Hands out exp(-a^2/2) and -Q.
 template <bool FINE>
 __device__ __forceinline__ void tails(F2 a, F2* e, F2* q) {
   float x, y;
@@ -206,23 +204,12 @@ __device__ __forceinline__ void act2(float& z0, float& z1) {
   if constexpr (ACT == LBP_ACT_RELU) {
     z0 = at_least(z0, 0.f);
     z1 = at_least(z1, 0.f);
-  } else if constexpr (ACT == LBP_ACT_GELU && FINE) {
+  } else if constexpr (ACT == LBP_ACT_GELU) {
+    // (the factor a makes gelu(0) zero and keeps the error near zero relative; a NaN comes through it)
     const F2 a = two(at_most(fabsf(z0), 100.f), at_most(fabsf(z1), 100.f));
     F2 e, q;
-    tails<true>(a, &e, &q);
-    parts(fma2(a, mul2(e, q), two(fmaxf(z0, 0.f), fmaxf(z1, 0.f))), z0, z1);   // (a NaN comes through a)
-  } else if constexpr (ACT == LBP_ACT_GELU) {
-    const F2 t = two(rcp(fmaf(0.4f, fabsf(z0), 1.f)), rcp(fmaf(0.4f, fabsf(z1), 1.f)));
-    const F2 z = two(z0, z1);
-    float e0, e1;
-    parts(mul2(z, mul2(z, two(-0.5f * kLog2e))), e0, e1);
-    F2 q = fma2(t, two(0.2135479748249054f), two(-0.5766780972480774f));
-    q = fma2(q, t, two(0.06343623995780945f));
-    q = fma2(q, t, two(-0.10194139182567596f));
-    q = fma2(q, t, two(0.0027213171124458313f));
-    q = fma2(q, t, two(0.3989139497280121f));
-    // (a NaN comes through the exponential)
-    parts(fma2(q, two(-ex2(e0), -ex2(e1)), two(fmaxf(z0, 0.f), fmaxf(z1, 0.f))), z0, z1);
+    tails<FINE>(a, &e, &q);
+    parts(fma2(a, mul2(e, q), two(fmaxf(z0, 0.f), fmaxf(z1, 0.f))), z0, z1);
   } else if constexpr (ACT == LBP_ACT_GELU_TANH || ACT == LBP_ACT_SILU) {
     // z / (1 + exp(-u))
     constexpr float kLeast = ACT == LBP_ACT_SILU ? -100.f : -30.f;   // (the result is 0 there)
