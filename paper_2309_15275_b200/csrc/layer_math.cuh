@@ -245,13 +245,16 @@ __device__ __forceinline__ void times_slope2(float& g0, float& g1, float z0, flo
     g0 = a > 0.f ? g0 : a;   // (0, or NaN)
     g1 = b > 0.f ? g1 : b;
   } else if constexpr (ACT == LBP_ACT_GELU) {
-    // Phi(z) + z phi(z) = 1/2 + sign(z) d, d = 1/2 - exp(-a^2/2) (Q - a / sqrt(2 pi)) >= 0, a = |z|
+    // Phi(z) + z phi(z) is h = exp(-a^2/2) (Q - a / sqrt(2 pi)) for z < 0, a = |z|, and 1 - h from zero on.  (Both
+    // from 1/2 - h, h would be rounded to a unit of 1/2: 4 % off at -5.5, nothing left at -7.)
     const F2 a = two(at_most(fabsf(z0), 100.f), at_most(fabsf(z1), 100.f));
     F2 e, q;
     tails<FINE>(a, &e, &q);
-    float x, y;
-    parts(fma2(e, fma2(a, two(kInvSqrt2Pi), q), two(0.5f)), x, y);
-    parts(mul2(two(g0, g1), add2(two(copysignf(x, z0), copysignf(y, z1)), two(0.5f))), g0, g1);
+    const F2 minus_h = mul2(e, fma2(a, two(kInvSqrt2Pi), q));
+    float h0, h1, r0, r1;
+    parts(minus_h, h0, h1);
+    parts(add2(minus_h, two(1.f)), r0, r1);
+    parts(mul2(two(g0, g1), two(z0 < 0.f ? -h0 : r0, z1 < 0.f ? -h1 : r1)), g0, g1);
   } else if constexpr (ACT == LBP_ACT_GELU_TANH || ACT == LBP_ACT_SILU) {
     constexpr float kMost = ACT == LBP_ACT_SILU ? 100.f : 12.f;   // (s is 0 and 1 there)
     const F2 c = two(clamp_abs(z0, kMost), clamp_abs(z1, kMost));

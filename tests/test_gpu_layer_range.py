@@ -60,3 +60,22 @@ def test_activations_near_zero(dev, dtype, a, rows, Cin, Cout):
         off, own = np.abs(f64(y) - want), HALF[dtype] + (2.0 ** -12 if dtype == torch.bfloat16 else 2.0 ** -20)
         assert np.all(off <= own * np.abs(want)), (p, float(np.max(off / np.maximum(np.abs(want), 1e-300))))
         assert torch.equal(lbp.lbp_linear(x, w, activation=a, p=p, seed=7, offset=4), y)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_slope_of_gelu_in_its_negative_tail(dev, dtype):
+    """Phi(z) + z phi(z) for -12 <= z <= -1, away from its zero at -0.75: no absolute error.
+
+    It is exp(-a^2/2) (Q - a / sqrt(2 pi)).  Q is off by at most 4e-7 (fp32) or 3.7e-5 (bf16) of itself, which at -1, where
+    the difference is smallest beside Q (0.137 and 0.262), is 2^-20 and 2^-13.7 of the result; the exponent's two roundings are
+    at most a^2 2^-24, the constant's and the exponential's own a^2 2^-25 and 2^-22."""
+    z = torch.linspace(-12, -1, 49152 * 8, dtype=torch.float64).view(-1, 512).to(dtype)
+    g = torch.where(torch.arange(z.numel()).view_as(z) % 3 == 0, -0.75, 1.0).to(dtype)
+    zz = f64(z)
+    for p in (0.0, 0.4):
+        want = Y.drop(f64(g), Y.row_numbers(*z.shape), p, 3, 8) * Y.act_slope(zz, "gelu")
+        got = f64(lbp.lbp_linear_grad(g.cuda(), z.cuda(), activation="gelu", p=p, seed=3, offset=8))
+        own = 2.0 ** -12 if dtype == torch.bfloat16 else 2.0 ** -19 * (1 + zz * zz)
+        off = np.abs(got - want)
+        assert np.all(off <= (HALF[dtype] + own) * np.abs(want)), (p, float(np.max(off / np.maximum(np.abs(want), 1e-300))))
+        assert np.all(got[want != 0] != 0)
