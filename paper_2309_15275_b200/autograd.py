@@ -45,7 +45,9 @@ class LbpLinear(torch.nn.Module):
     `activation` (one of `ACTIVATIONS`), `dropout` (the probability, drawn from torch's
     generator of the device while the module is in training mode) and the `residual` given
     to a call are applied in the product's epilogue.  Such a call wants CUDA tensors of one
-    dtype (fp32 or bf16; under autocast everything is cast to its type).  A backward pass
+    dtype, fp32 or bf16.  Under autocast x, weight and bias are cast to its type, as by torch's
+    own linear layer; a residual of another type keeps it and is added to the result by
+    torch's rules (fp32 onto bf16: fp32).  A backward pass
     can be captured into a graph like that of torch's own layers, and under the same
     condition: no graph of earlier, uncaptured passes over the same parameters is alive.
     """

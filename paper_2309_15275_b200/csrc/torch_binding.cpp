@@ -1118,22 +1118,37 @@ PyObject* py_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
     TORCH_CHECK_VALUE(H == 0 || (x.dim() == 3 && x.size(1) >= static_cast<int64_t>(H) * W),
                       "with a grid, x must be (B, n + H*W, Cin)");
     TORCH_CHECK_VALUE(H > 0 || x.dim() == 4, "x must be (B, H, W, Cin)");
-    // under autocast everything is of its type, as for torch's own product
+    const auto opt = [](const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; };
+    // Under autocast the product's operands and the bias are of its type, as for torch's own linear layer.  A residual
+    // stream keeps its own, and the sum with it follows torch's rules, as it does behind torch's layer.
+    Tensor stream;
     if (at::autocast::is_autocast_enabled(at::kCUDA)) {
       const at::ScalarType t = at::autocast::get_autocast_dtype(at::kCUDA);
-      for (Tensor* v : {&x, &weight, &bias, &residual})
-        if (v->defined() && v->is_floating_point()) *v = v->to(t);
+      if (residual.defined() && residual.scalar_type() != t) {
+        c10::SmallVector<int64_t, 8> shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = weight.dim() == 2 ? weight.size(0) : -1;
+        TORCH_CHECK_VALUE(residual.is_floating_point() && residual.sizes() == shape && residual.device() == x.device(),
+                          "LbpLinear: residual ", residual.sizes(), " ", residual.scalar_type(), " on ", residual.device(),
+                          " must have the output's shape ", at::IntArrayRef(shape), " and device");
+        std::swap(stream, residual);
+      }
+      if (!stream.defined() || act != LBP_ACT_NONE || p > 0.0)
+        for (Tensor* v : {&x, &weight, &bias})
+          if (v->defined() && v->is_floating_point()) *v = v->to(t);
     }
-    const auto opt = [](const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; };
     bool backward = false;
     if (at::GradMode::is_enabled())
       for (const Tensor* v : {&x, &weight, &bias, &residual}) backward |= v->defined() && v->requires_grad();
-    if (backward)
+    if (stream.defined() && act == LBP_ACT_NONE && p == 0.0)   // nothing else follows the product: the plain layer's
+      y = LinearFunction::apply(x, weight, opt(bias), static_cast<int64_t>(k), flat, projected, static_cast<int64_t>(H),
+                                static_cast<int64_t>(W));
+    else if (backward)
       y = LayerFunction::apply(x, weight, opt(bias), opt(residual), static_cast<int64_t>(k), flat, projected,
                                static_cast<int64_t>(H), static_cast<int64_t>(W), static_cast<int64_t>(act), p);
     else
       y = LayerFunction::compute(x, weight, opt(bias), opt(residual), act, p, p > 0.0 ? draw_state(x.get_device()) : Drawn{},
                                  nullptr, nullptr);
+    if (stream.defined()) y = stream + y;
   }
   return wrap_like(y, a, 4);
   END_HANDLE_TH_ERRORS

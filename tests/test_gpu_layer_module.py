@@ -1,0 +1,61 @@
+"""LbpLinear with an epilogue among torch's own mechanisms: autocast and forward-mode derivatives."""
+import pytest
+import torch
+
+import paper_2309_15275_b200 as lbp
+from oracle import lbp_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+K, BASES = 8, O.select_bases(8, O.RULE_PREFIX, 8)
+EPILOGUES = [dict(activation="gelu", dropout=0.2), dict(dropout=0.3), dict(activation="silu"), dict()]
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    return torch.device("cuda:0")
+
+
+def _normal(shape, std, dtype, seed):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("epilogue", EPILOGUES)
+@pytest.mark.parametrize("cls", [None, 0, 1, 2])
+def test_a_residual_stream_keeps_its_type_under_autocast(dev, epilogue, cls):
+    """torch's rule for the sum: fp32 onto bf16 is fp32, with not a bit of the stream lost.  The terms are those of the call
+    without a residual, so y, and every gradient, is what torch's own sum behind that call gives."""
+    seq = () if cls is None else (cls + 64,)
+    shape = (3, 8, 8) if cls is None else (3,) + seq
+    layer = lbp.LbpLinear(64, 96, K, BASES, device=dev, dtype=torch.float32, bias=True, grid=None if cls is None else (8, 8), **epilogue)
+    with torch.no_grad():
+        layer.bias.normal_(0, 0.3)
+    x = _normal(shape + (64,), 1.0, torch.float32, 1).requires_grad_()
+    r = _normal(shape + (96,), 1.0, torch.float32, 2).requires_grad_()
+    g = _normal(shape + (96,), 1.0, torch.float32, 3)
+    leaves = (x, layer.weight, layer.bias, r)
+
+    def run(step):
+        torch.manual_seed(11)
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            y = step()
+        return y, torch.autograd.grad(y, leaves, g)
+
+    want, want_grads = run(lambda: r + layer(x))
+    y, grads = run(lambda: layer(x, residual=r))
+    assert want.dtype == y.dtype == torch.float32 and torch.equal(y, want)
+    assert torch.equal(grads[3], g) and all(torch.equal(a, b) for a, b in zip(grads, want_grads))
+    with torch.no_grad():     # and where nothing is to be differentiated
+        torch.manual_seed(11)
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            assert torch.equal(layer(x, residual=r), want)
+            # a residual of autocast's own type still rides in the epilogue
+            low = layer(x, residual=r.bfloat16())
+            assert low.dtype == torch.bfloat16 and low.shape == y.shape
+            for bad in (r[..., :1], r[:1], r.long(), r.cpu()):
+                with pytest.raises(ValueError):
+                    layer(x, residual=bad)
+    with pytest.raises(ValueError):   # without autocast one dtype, as before
+        layer(x, residual=r.bfloat16())
