@@ -50,6 +50,7 @@ class LbpLinear(torch.nn.Module):
     torch's rules (fp32 onto bf16: fp32).  A backward pass
     can be captured into a graph like that of torch's own layers, and under the same
     condition: no graph of earlier, uncaptured passes over the same parameters is alive.
+    There is no forward-mode derivative: an operand with a tangent is refused.
     """
 
     activation, dropout = None, 0.0     # (also of modules stored before there were these)

@@ -1115,6 +1115,10 @@ PyObject* py_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
     pybind11::gil_scoped_release no_gil;
     TORCH_CHECK_VALUE(x.is_cuda(), "x must be a CUDA tensor (the library has no CPU path)");
     TORCH_CHECK_VALUE(p >= 0.0 && p <= 1.0, "dropout is a probability, got ", p);
+    // (the calls below that go past the autograd function would leave a tangent behind)
+    for (const Tensor* v : {&x, &weight, &bias, &residual})
+      TORCH_CHECK_NOT_IMPLEMENTED(!v->defined() || !v->_fw_grad(/*level=*/0).defined(),
+                                  "LbpLinear has no forward-mode derivative");
     TORCH_CHECK_VALUE(H == 0 || (x.dim() == 3 && x.size(1) >= static_cast<int64_t>(H) * W),
                       "with a grid, x must be (B, n + H*W, Cin)");
     TORCH_CHECK_VALUE(H > 0 || x.dim() == 4, "x must be (B, H, W, Cin)");

@@ -59,3 +59,24 @@ def test_a_residual_stream_keeps_its_type_under_autocast(dev, epilogue, cls):
                     layer(x, residual=bad)
     with pytest.raises(ValueError):   # without autocast one dtype, as before
         layer(x, residual=r.bfloat16())
+
+
+@pytest.mark.parametrize("epilogue", EPILOGUES)
+@pytest.mark.parametrize("frozen", [False, True])
+@pytest.mark.parametrize("with_grad", [False, True])
+def test_tangents_are_refused_and_not_lost(dev, epilogue, frozen, with_grad):
+    """There is no forward-mode derivative; a call that went on without the tangent would answer zero for it."""
+    from torch.autograd import forward_ad
+    layer = lbp.LbpLinear(64, 64, K, BASES, device=dev, dtype=torch.float32, bias=True, **epilogue)
+    layer.requires_grad_(not frozen)
+    x, r = (_normal((1, 8, 8, 64), 1.0, torch.float32, s) for s in (1, 2))
+    before = torch.cuda.default_generators[0].get_offset()
+    with torch.set_grad_enabled(with_grad), forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: layer(dual), lambda: layer(dual, residual=r), lambda: layer(x, residual=dual)):
+            with pytest.raises(RuntimeError, match="forward-mode|jvp"):
+                call()
+            with torch.autocast("cuda", dtype=torch.bfloat16), pytest.raises(RuntimeError, match="forward-mode|jvp"):
+                call()
+        assert layer(x, residual=r).shape == x.shape     # without one it goes on as ever
+    assert torch.cuda.default_generators[0].get_offset() == before + (4 if epilogue.get("dropout") else 0)
