@@ -337,6 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if constexpr (ZY) put(true, h, zw);
           put(false, h, w);
+          if constexpr (RES) __syncwarp();   // (rows past the last read nothing: together again for the accumulator)
         };
         auto send = [&](int from) {   // the box, whose channels begin `from` further on
           ptx::fence_proxy_async_smem();
@@ -348,6 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             bulk_commit();
           }
+          __syncwarp();   // what follows reads the accumulator, with all lanes at once
         };
         uint32_t a0[16];
         if constexpr (DROP && RES) {   // (the registers are needed otherwise)
