@@ -15,9 +15,10 @@ pytestmark = pytest.mark.gpu
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
 DTYPES = [torch.bfloat16, torch.float32]
 ACTS = ["relu", "gelu", "gelu_tanh", "silu"]
-# rows, Cin, Cout: every form of lbp_linear.  bf16: 8 and 16 tokens, K shared in a cluster, a CTA a tile, CTA pairs; fp32:
-# few tokens, one tile and several to a CTA.
-FORMS = [(5, 64, 128), (12, 64, 128), (100, 128, 192), (1000, 128, 64), (1000, 192, 512), (20000, 64, 128)]
+# rows, Cin, Cout: every form of lbp_linear.  bf16: up to 8 and 16 tokens, a CTA a tile, K shared among four and two CTAs of a
+# cluster, CTA pairs; fp32: few tokens, one tile and several to a CTA.
+FORMS = [(5, 64, 128), (12, 64, 128), (100, 128, 192), (100, 1024, 192), (1000, 2304, 768), (1000, 128, 64), (1000, 192, 512),
+         (20000, 64, 128)]
 
 
 @pytest.fixture(scope="module")
