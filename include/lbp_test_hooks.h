@@ -25,7 +25,8 @@ extern "C" {
  * `on`: bit 0 stalls the products kernels as described; bit 1 does the same to
  * the TMA producers of the tcgen05 projection kernel (orders 8 and 16, bf16, r <= 48:
  * lbp_project and the first kernel of lbp_backward); bit 2 to the loads of the fp32
- * products on the tensor cores; bit 3 to those of lbp_linear on bf16 data; 0 switches all off.
+ * products on the tensor cores; bit 3 to those of lbp_linear on bf16 data.  With bit 4
+ * those of bits 1 and 3 fetch a first block and stop behind it.  0 switches all off.
  * Returns LBP_OK. */
 int lbp_test_stall_products(int on);
 

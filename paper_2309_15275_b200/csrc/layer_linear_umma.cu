@@ -105,6 +105,20 @@ struct Walk {
   }
 };
 
+// After an expired wait, one thread: the MMAs of the first `mmas` blocks and the loads of the first `loads` have ended, or
+// another wait has run out, before memory that they touch is given back.  (Earlier uses of a stage have ended: its later
+// ones waited for them.)
+__device__ __forceinline__ void settle(uint64_t* full, uint64_t* empty, int stages, int loads, int mmas, uint32_t* status) {
+  if (mmas > 0) ptx::mbar_wait_parked(&empty[(mmas - 1) % stages], ((mmas - 1) / stages) & 1u, status, kSite | 5u);
+  for (int u = loads > stages ? loads - stages : 0; u < loads; ++u)
+    if (!ptx::mbar_wait_parked(&full[u % stages], (u / stages) & 1u, status, kSite | 6u)) return;
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, int v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+// Blocks that are fetched while a test stalls the loads (0: it does not).
+__device__ __forceinline__ int most_loads(int test_stall) { return test_stall == 0 ? 0x7fffffff : test_stall - 1; }
+
 template <int ACT, bool DROP, bool RES, bool ZY, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_umma_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
@@ -118,6 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* const acc_empty = acc_full + 2;         // [2], the leader's are used
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* const counts = abort_flag + 1;      // [3]: blocks loaded by the leader, by its peer; blocks multiplied
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? static_cast<int>(ptx::cluster_ctarank()) : 0;
@@ -134,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     ptx::mbar_fence_init();
     *abort_flag = 0;
+    counts[0] = counts[1] = counts[2] = 0;
     ptx::prefetch_tensormap(&tm.x);
     ptx::prefetch_tensormap(&tm.W);
   }
@@ -161,13 +177,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t keep = ptx::l2_policy_evict_last();
       const int part = p.BN / kCtas;   // W's rows of this CTA
       const uint32_t tx = static_cast<uint32_t>(kCtas * (kABytes + part * kBK * 2));
-      int s = 0;
+      int s = 0, loads = 0;
       uint32_t phase = 0;
       bool ok = true;
+      const int most = most_loads(p.test_stall);
       Walk at(p, unit, units);
-      for (int t = unit; t < p.tiles && ok && !p.test_stall; t += units, at.advance(p)) {
+      for (int t = unit; t < p.tiles && ok && loads < most; t += units, at.advance(p)) {
         const int row = (at.m * kCtas + rank) * kBM, col = at.n * p.BN + rank * part;
-        for (int kb = 0; kb < p.num_kb; ++kb) {
+        for (int kb = 0; kb < p.num_kb && loads < most; ++kb) {
           if (!ptx::mbar_wait_parked(&empty[s], phase ^ 1u, p.status, kSite | 1u)) {
             ok = false;
             break;
@@ -182,12 +199,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             ptx::tma_load_2d_hint(sa, &tm.x, &full[s], kb * kBK, row, keep);
             ptx::tma_load_2d_hint(sa + kABytes, &tm.W, &full[s], kb * kBK, col, keep);
           }
+          ++loads;
           if (++s == p.stages) {
             s = 0;
             phase ^= 1u;
           }
         }
       }
+      if (PAIR && rank != 0)
+        store_cluster(ptx::map_to_rank(ptx::smem_u32(const_cast<int*>(counts + 1)), 0), loads);
+      else
+        counts[0] = loads;
       if (!ok) *abort_flag = 1;
     }
   } else if (warp == 1) {
@@ -200,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         else
           ptx::mma_commit(bar);
       };
-      int s = 0, n = 0;
+      int s = 0, n = 0, mmas = 0;
       uint32_t phase = 0;
       bool ok = true;
       for (int t = unit; t < p.tiles && ok; t += units, ++n) {
@@ -226,6 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               ptx::mma_bf16_ss(d, da, db, idesc, add);
           }
           commit(&empty[s]);
+          ++mmas;
           if (++s == p.stages) {
             s = 0;
             phase ^= 1u;
@@ -233,6 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok) commit(&acc_full[n & 1]);
       }
+      counts[2] = mmas;
       if (!ok) *abort_flag = 1;
     }
   } else {
@@ -395,7 +419,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if constexpr (PAIR) ptx::cluster_sync_all();   // neither CTA leaves while the other may still touch its memory
+  if constexpr (PAIR) {
+    if (threadIdx.x == 0 && *abort_flag != 0)
+      store_cluster(ptx::map_to_rank(ptx::smem_u32(const_cast<int*>(abort_flag)), rank ^ 1), 1);
+    ptx::cluster_sync_all();   // neither CTA leaves while the other may still touch its memory
+  }
+  if (*abort_flag != 0) {   // (the same in both CTAs; the pair's loads and MMAs signal on the leader's barriers)
+    if (rank == 0 && threadIdx.x == 0)
+      settle(full, empty, p.stages, counts[0] > counts[1] ? counts[0] : counts[1], counts[2], p.status);
+    __syncthreads();
+    if constexpr (PAIR) ptx::cluster_sync_all();
+  }
   if (warp == 1) {
     ptx::tc_fence_after_sync();
     if constexpr (PAIR)
@@ -432,6 +466,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   uint64_t* const empty = full + kSplitStages;
   uint64_t* const acc_full = empty + kSplitStages;
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* const counts = abort_flag + 1;   // [2]: blocks loaded, multiplied
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = static_cast<int>(ptx::cluster_ctarank()), tile = blockIdx.x / S;
   const int m = tile / p.tiles_n, col0 = (tile - m * p.tiles_n) * BN;
@@ -444,6 +480,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     }
     ptx::mbar_init(acc_full, 1);
     ptx::mbar_fence_init();
+    *abort_flag = counts[0] = counts[1] = 0;
     ptx::prefetch_tensormap(&tm.x);
     ptx::prefetch_tensormap(&tm.W);
   }
@@ -461,20 +498,27 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     if (ptx::elect_one()) {
       asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
       const uint64_t keep = ptx::l2_policy_evict_last();
-      for (int kb = kb0, i = 0; kb < kb1 && !p.test_stall; ++kb, ++i) {
+      const int most = most_loads(p.test_stall);
+      int i = 0;
+      for (int kb = kb0; kb < kb1 && i < most; ++kb, ++i) {
         const int s = i % kSplitStages;
-        if (!ptx::mbar_wait_parked(&empty[s], ((i / kSplitStages) + 1) & 1u, p.status, kSite | 7u)) break;
+        if (!ptx::mbar_wait_parked(&empty[s], ((i / kSplitStages) + 1) & 1u, p.status, kSite | 7u)) {
+          *abort_flag = 1;
+          break;
+        }
         uint8_t* const sa = smem + s * stage_bytes;
         ptx::mbar_expect_tx(&full[s], stage_bytes);
         ptx::tma_load_2d_hint(sa, &tm.x, &full[s], kb * kBK, m * kBM, keep);
         ptx::tma_load_2d_hint(sa + kABytes, &tm.W, &full[s], kb * kBK, col0, keep);
       }
+      counts[0] = i;
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
       const uint32_t idesc = ptx::idesc_bf16(kBM, BN, false, false);
       bool ok = true;
-      for (int kb = kb0, i = 0; kb < kb1 && ok; ++kb, ++i) {
+      int i = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++i) {
         const int s = i % kSplitStages;
         ok = ptx::mbar_wait_parked(&full[s], (i / kSplitStages) & 1u, p.status, kSite | 8u);
         if (!ok) break;
@@ -486,7 +530,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
                            idesc, (i == 0 && kk == 0) ? 0u : 1u);
         ptx::mma_commit(&empty[s]);
       }
-      if (ok) ptx::mma_commit(acc_full);
+      counts[1] = i;
+      if (ok)
+        ptx::mma_commit(acc_full);
+      else
+        *abort_flag = 1;
     }
   }
   const int quarter = warp & 3, row = quarter * 32 + lane, half = (warp - 2) >> 2;   // warps 2-9: a row of the tile a thread, every other 16 columns
@@ -494,7 +542,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   if (warp >= 2) {
     // (a CTA without k-blocks, where they do not share out evenly, has zeros)
     bool ok = kb0 < kb1;
-    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait_parked(acc_full, 0, p.status, kSite | 9u));
+    if (ok) {
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait_parked(acc_full, 0, p.status, kSite | 9u));
+      if (!ok) *abort_flag = 1;
+    }
     ptx::tc_fence_after_sync();
 #pragma unroll 1
     for (int c = half * 16; c < BN; c += 32) {
@@ -513,6 +564,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
+  if (*abort_flag != 0) {
+    if (threadIdx.x == 0) settle(full, empty, kSplitStages, counts[0], counts[1], p.status);
+    __syncthreads();
+  }
   ptx::cluster_sync_all();
   if (warp == 1) {
     ptx::tc_fence_after_sync();
@@ -639,7 +694,7 @@ Plan choose_plan(const LinearCall& c, int sms) {
 
 }  // namespace
 
-static thread_local bool g_test_stall = false;
+static thread_local int g_test_stall = 0;
 
 int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   int dev = 0, sms = 0;
@@ -660,7 +715,7 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
   p.stage_bytes = kABytes + part * kBK * 2;
   const int room = kSmemMax - kBarBytes - kBiasBytes - kOutBytes;
   p.stages = room / p.stage_bytes < kMaxStages ? room / p.stage_bytes : kMaxStages;
-  p.test_stall = g_test_stall ? 1 : 0;
+  p.test_stall = g_test_stall;
   p.first = c.first;
   p.step = c.step;
   p.drop = c.drop;
@@ -737,6 +792,6 @@ int launch_linear_umma(const LinearCall& c, cudaStream_t stream) {
 
 }  // namespace layer
 
-void set_test_stall_linear(bool on) { layer::g_test_stall = on; }
+void set_test_stall_linear(int mode) { layer::g_test_stall = mode; }
 
 }  // namespace lbp

@@ -376,9 +376,9 @@ const FusedOverlap* fused_overlap() { return g_overlap; }
 static thread_local bool g_test_stall = false;
 void set_test_stall(bool on) { g_test_stall = on; }
 bool test_stall() { return g_test_stall; }
-static thread_local bool g_test_stall_projection = false;
-void set_test_stall_projection(bool on) { g_test_stall_projection = on; }
-bool test_stall_projection() { return g_test_stall_projection; }
+static thread_local int g_test_stall_projection = 0;
+void set_test_stall_projection(int mode) { g_test_stall_projection = mode; }
+int test_stall_projection() { return g_test_stall_projection; }
 
 static long long grid_blocks(const lbp_layer& L) {
   return static_cast<long long>(L.B) * blocks_along(L.H, L.k) * blocks_along(L.W, L.k);

@@ -133,7 +133,7 @@ int launch_project(const void* t, void* t_hat, int dtype, int B, int H, int W, i
                    float scale = 0.f, const lbp_view* view = nullptr);
 
 // Per-thread switch read by the projection launchers (umma::Params::defer_wait).
-bool test_stall_projection();   // test hook (lbp_fused.cu)
+int test_stall_projection();   // test hook (lbp_fused.cu): 0, or 1 + the loads that are issued all the same
 void set_projection_defer_wait(bool on);
 bool projection_defer_wait();
 
@@ -194,7 +194,7 @@ int launch_gemm_fp32(const GemmFp32* jobs, int n, float* ws, size_t ws_bytes, ui
 // Scratch for the K slices these take at best (with less, K is sliced less or not at all).
 size_t gemm_fp32_ws_bytes(const GemmFp32* jobs, int n);
 void set_test_stall_fp32(bool on);   // test hook (gemm_fp32_split.cu)
-void set_test_stall_linear(bool on);   // test hook (layer_linear_umma.cu)
+void set_test_stall_linear(int mode);   // test hook (layer_linear_umma.cu): as test_stall_projection
 void gemm_fp32_plan(const GemmFp32 (&jobs)[2], size_t room, int64_t* out6);   // test hook
 size_t gemm_splitk_ws_bytes(long long M, long long N, long long K, int in_dtype);
 // D[i] = beta * D[i] + sum over `splits` fp32 planes of mn elements each (mn a multiple

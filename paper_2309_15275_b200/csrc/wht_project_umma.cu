@@ -61,7 +61,7 @@ constexpr int kFirstEpilogue = GRAD ? 3 : 8;     // (GRAD has no warp to spare: 
 template <bool GRAD>
 constexpr int kThreadsOf = (kFirstEpilogue<GRAD> + (GRAD ? 4 + kGradWarps : 4 * kMaxGroups)) * 32;
 constexpr int kMaxStages = 6;
-constexpr int kBarBytes = 256;
+constexpr int kBarBytes = 256;                   // barriers (216 bytes with GRAD), counters
 constexpr int kSmemMax = 227 * 1024;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kSlots = 4;                        // accumulator slots (items in flight)
@@ -245,6 +245,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
   uint64_t* ready_bar = acc_empty + kSlots;      // [kMaxStages], GRAD: g_z is in place
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ready_bar + (GRAD ? kMaxStages : 0));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* counts = tmem_slot + 2;              // [2]: stages that have been loaded, and multiplied
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -264,6 +265,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
     }
     ptx::mbar_fence_init();
     *abort_flag = 0;
+    counts[0] = counts[1] = 0u;
   }
   if (warp == kMma) {
     ptx::tmem_alloc(tmem_slot, kTmemCols);
@@ -331,9 +333,10 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       for (int q = 0; q < kMine; ++q) cs[q].decode(p, 4 * blockIdx.x + warp + q * kProd);
       bool ok = true;
       int s = 0;
-      uint32_t phase = 0;
-      for (uint32_t n = 0; n < my_items && !p.test_stall && ok; ++n) {
-        for (int part = 0; part < kParts; ++part) {
+      uint32_t phase = 0, loads = 0;
+      const uint32_t most = p.test_stall == 0 ? ~0u : static_cast<uint32_t>(p.test_stall - 1);
+      for (uint32_t n = 0; n < my_items && loads < most && ok; ++n) {
+        for (int part = 0; part < kParts && loads < most; ++part) {
           if (!wait<GRAD>(&empty_bar[s], phase ^ 1u, p.status, (6u << 16) | 1u)) {
             ok = false;
             break;
@@ -365,6 +368,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
               if (with_z && c.which == 0) fetch(&grad.z, smem + s * stage_bytes + kStageBytes);
             }
           }
+          ++loads;
           if (++s == p.stages) {
             s = 0;
             phase ^= 1u;
@@ -374,6 +378,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
         for (int q = 0; q < kMine; ++q)
           if (ok && n + 1 < my_items) cs[q].advance(p, stride);
       }
+      atomicMax(&counts[0], loads);
       if (!ok) *abort_flag = 1;
     }
   } else if (warp == kMma) {
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
       const uint32_t b_addr = ptx::smem_u32(sB);
       bool ok = true;
       int s = 0;
-      uint32_t phase = 0;
+      uint32_t phase = 0, mmas = 0;
       for (uint32_t n = 0; n < my_items && ok; ++n) {
         const int slot = static_cast<int>(n % kSlots);
         const bool second = 4 * (blockIdx.x + n * gridDim.x) + 2 < p.n_chunks;   // of the two halves of an item
@@ -412,6 +417,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
             }
           }
           ptx::mma_commit(&empty_bar[s]);
+          ++mmas;
           if (++s == p.stages) {
             s = 0;
             phase ^= 1u;
@@ -420,6 +426,7 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
         if (!ok) break;
         ptx::mma_commit(&acc_full[slot]);
       }
+      counts[1] = mmas;
       if (!ok) *abort_flag = 1;
     }
   } else if (GRAD && warp >= kEpi + 4) {
@@ -555,6 +562,18 @@ __global__ void __launch_bounds__(kThreadsOf<std::is_same<G, Grad>::value>, 1)
 
   ptx::tc_fence_before_sync();
   __syncthreads();
+  if (*abort_flag != 0) {
+    // After an expired wait the MMAs and loads under way end first, or another wait runs out.  (Earlier uses of a stage
+    // have ended: its later ones waited for them.)
+    if (threadIdx.x == 0) {
+      const uint32_t stages = static_cast<uint32_t>(p.stages), loads = counts[0], mmas = counts[1];
+      if (mmas > 0) wait<GRAD>(&empty_bar[(mmas - 1) % stages], ((mmas - 1) / stages) & 1u, p.status, (6u << 16) | 6u);
+      bool ok = true;
+      for (uint32_t u = loads > stages ? loads - stages : 0u; u < loads && ok; ++u)
+        ok = wait<GRAD>(&full_bar[u % stages], (u / stages) & 1u, p.status, (6u << 16) | 7u);
+    }
+    __syncthreads();
+  }
   if (warp == kMma) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tmem_base, kTmemCols);
@@ -618,7 +637,7 @@ int launch_project_umma(const void* t0, void* out0, int C0, const lbp_view* view
   p.scale[0] = scale0;
   p.scale[1] = scale1;
   p.defer_wait = projection_defer_wait() ? 1 : 0;
-  p.test_stall = test_stall_projection() ? 1 : 0;
+  p.test_stall = test_stall_projection();
 
   MmaPlan mp;
   for (int q = 0; q < 64; ++q) {
