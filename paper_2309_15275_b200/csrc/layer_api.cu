@@ -14,8 +14,25 @@ static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 static const lbp_epilogue kNoEpilogue{};
 static const lbp_pitches kDense{};
 
-// The numbers of a call's elements are below 2^62, so that no sum here overflows.
+// The numbers of a call's elements are below 2^62, so that no sum in a kernel overflows.
 constexpr int64_t kMostElements = int64_t{1} << 62;
+// How many elements (places or numbers) there are from the first to the last of `count` steps along each of three strides,
+// C of them behind the last.  (Up to 2^91.)
+struct Steps3 {
+  long long count[3];
+  int64_t stride[3];
+};
+static __int128 extent(const Steps3& s, int C) {
+  __int128 n = C;
+  for (int i = 0; i < 3; ++i)
+    if (s.count[i] > 0) n += static_cast<__int128>(s.count[i] - 1) * s.stride[i];
+  return n;
+}
+static int check_numbers(int64_t first, const Steps3& s, int C) {
+  return first + extent(s, C) > kMostElements ? LBP_ERR_SHAPE : LBP_OK;
+}
+static Steps3 along_rows(long long rows, int64_t pitch) { return Steps3{{rows, 0, 0}, {pitch, 0, 0}}; }
+static Steps3 along_grid(int B, int H, int W, const lbp_view& v) { return Steps3{{B, H, W}, {v.image, v.row, v.token}}; }
 
 static int check_rows(long long rows, int C, int dtype) {
   if (dtype != LBP_F32 && dtype != LBP_BF16) return LBP_ERR_DTYPE;
@@ -111,6 +128,7 @@ static int check_pointwise(const void* a, const void* b, bool need_b, const void
                            const lbp_pitches& p, int64_t pa, int64_t pb, int64_t po, const lbp_epilogue& e) {
   if (int s = check_rows(rows, C, dtype)) return s;
   if (int s = check_epilogue(e, dtype)) return s;
+  if (int s = check_numbers(e.first, along_rows(rows, e.number.token ? e.number.token : C), C)) return s;
   for (int64_t v : {p.x, p.residual, p.y, p.z})
     if (int s = check_pitch(v, C, dtype)) return s;
   if (rows == 0) return LBP_OK;
@@ -215,6 +233,7 @@ int lbp_linear(const void* x, const void* W, const void* bias, const void* resid
   if (int s = check_rows(rows, Cin, dtype)) return s;
   if (int s = check_rows(rows, Cout, dtype)) return s;
   if (int s = check_epilogue(e, dtype)) return s;
+  if (int s = check_numbers(e.first, along_rows(rows, e.number.token ? e.number.token : Cout), Cout)) return s;
   if (int s = check_pitch(p.x, Cin, dtype)) return s;
   for (int64_t v : {p.residual, p.y, p.z})
     if (int s = check_pitch(v, Cout, dtype)) return s;
@@ -297,6 +316,7 @@ int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, 
   if (g_y == nullptr || t_hat == nullptr || (z == nullptr && e.act != LBP_ACT_NONE)) return LBP_ERR_NULL;
   if (int s = check_shape(B, H, W, C, k, dtype)) return s;
   if (int s = check_epilogue(e, dtype)) return s;
+  if (int s = check_numbers(e.first, along_grid(B, H, W, resolve_view(&e.number, H, W, C)), C)) return s;
   if (view != nullptr)
     if (int s = check_grid_view(*view, C, dtype)) return s;
   BasisPlan plan;
@@ -348,6 +368,9 @@ int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const vo
   if (int s = backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, true)) return s;
   const size_t need = lbp_workspace_bytes_act(layer, r, ex, x_hat != nullptr);
   if (!fits_grid(layer->H, layer->W)) return LBP_ERR_SHAPE;
+  if (int s = check_numbers(e.first, along_grid(layer->B, layer->H, layer->W, resolve_view(&e.number, layer->H, layer->W, C)), C))
+    return s;
+  if (int s = check_numbers(grad->first_extra, along_rows(n_extra, grad->number_extra ? grad->number_extra : C), C)) return s;
   if (need == 0 || ws_bytes < need) return LBP_ERR_WORKSPACE;
   if (int s = check_device_arch()) return s;
   if (does_nothing(e)) return backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, false);

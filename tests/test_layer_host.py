@@ -248,3 +248,39 @@ def test_sizes_past_the_kernels_integers_are_refused():
     lay = B._layer(1, 1 << 16, 1 << 15, 8, 8, 8, lbp.LBP_BF16, lbp.LBP_F32)
     assert B._lib().lbp_workspace_bytes_act(C.byref(lay), 4, None, 0) == 0
     assert _backward(lay=lay, n=1 << 50) == SHAPE
+
+
+FAR = 1 << 62
+
+
+@pytest.mark.parametrize("rows,first,step", [
+    ((1 << 18) + 1, 0, 1 << 45),                    # 2^63: past the kernels' signed sums
+    ((1 << 12) + 2, 0, (1 << 50) - 8), (2, FAR - 64 - 8, 64), (1, FAR - 56, 0), (1 << 40, 0, (1 << 50) - 8),
+])
+def test_numbers_past_2_62_are_refused(rows, first, step):
+    ep = _ep(first=first, number=B.View(0, 0, step))
+    assert _linear(rows=rows, Cout=64, ep=ep, n=1 << 60) == SHAPE
+    assert _pointwise("lbp_dropout", rows=rows, ep=ep) == _pointwise("lbp_linear_grad", rows=rows, ep=ep) == SHAPE
+
+
+@pytest.mark.parametrize("which", range(4))
+def test_numbers_of_a_grid_past_2_62_are_refused(which):
+    # along each of the strides, and of the first number alone
+    big = (1 << 50) - 8
+    view = [B.View(big, 64, 64), B.View(64, big, 64), B.View(64, 64, big), B.View(64, 64, 64)][which]
+    shape = [dict(B_=4100, H=1, W=1), dict(B_=1, H=4100, W=1), dict(B_=1, H=1, W=4100), dict(B_=1, H=1, W=1)][which]
+    ep = _ep(first=FAR - 56 if which == 3 else 0, number=view)
+    assert _project(ep=ep, **shape) == SHAPE
+    lay = B._layer(shape["B_"], shape["H"], shape["W"], 64, 64, 8, lbp.LBP_BF16, lbp.LBP_F32)
+    assert _backward(ep=ep, lay=lay) == SHAPE
+
+
+def test_the_last_number_below_2_62_is_accepted():
+    accepted = (8, 9)   # (what is left to fail is the machine without a device)
+    ep = _ep(first=FAR - 128, number=B.View(0, 0, 64))
+    assert _linear(rows=2, Cout=64, ep=ep) in accepted and _pointwise("lbp_dropout", rows=2, ep=ep) in accepted
+    # of extra tokens
+    big = (1 << 50) - 8
+    assert _backward(ex=_extra(n=4100), number_extra=big) == SHAPE
+    assert _backward(ex=_extra(n=3), number_extra=big) in accepted
+    assert _backward(ex=_extra(n=1), first_extra=FAR - 120) == SHAPE
