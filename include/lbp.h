@@ -310,7 +310,7 @@ int lbp_backward_fullrank(const void* x, const void* g_y, const void* W,
  * offsets give other, independent choices.
  *
  * A row has C elements; `pitch` arguments are distances between rows in elements
- * (0: dense rows, C), at least C and with the same alignment as pointers.  Rows of
+ * (0: dense rows, C), at least C, below 2^40 bytes and with the same alignment as pointers.  Rows of
  * one tensor may not overlap.  rows = 0 is a call that does nothing.  A row has at most
  * 2^30 elements and a grid fewer than 2^31 tokens an image (LBP_ERR_SHAPE). */
 typedef enum {

@@ -42,7 +42,7 @@ static int check_rows(long long rows, int C, int dtype) {
 }
 static int check_pitch(int64_t pitch, int C, int dtype) {
   if (pitch == 0) return LBP_OK;
-  if (pitch < C || pitch >= (int64_t{1} << 40)) return LBP_ERR_SHAPE;   // (a tensor map's stride)
+  if (pitch < C || pitch >= (int64_t{1} << 40) / elem_size(dtype)) return LBP_ERR_SHAPE;   // (a tensor map's stride: 2^40 bytes)
   return (pitch * elem_size(dtype)) % 16 != 0 ? LBP_ERR_ALIGN : LBP_OK;
 }
 static bool in_quads(int64_t v, int dtype) { return v % (dtype == LBP_BF16 ? 8 : 4) == 0; }

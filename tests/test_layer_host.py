@@ -284,3 +284,15 @@ def test_the_last_number_below_2_62_is_accepted():
     assert _backward(ex=_extra(n=4100), number_extra=big) == SHAPE
     assert _backward(ex=_extra(n=3), number_extra=big) in accepted
     assert _backward(ex=_extra(n=1), first_extra=FAR - 120) == SHAPE
+
+
+@pytest.mark.parametrize("dtype,es", [(lbp.LBP_BF16, 2), (lbp.LBP_F32, 4)])
+def test_pitches_past_a_tensor_maps_stride_are_refused(dtype, es):
+    """A stride of 2^40 bytes and more is the caller's mistake, not a failed CUDA call."""
+    accepted = (8, 9)   # (what is left to fail is the machine without a device)
+    for pitch, want in (((1 << 40) // es, (SHAPE,)), ((1 << 40) // es - 16, accepted)):
+        for name in ("x", "residual", "y", "z"):
+            p = B.Pitches(**{name: pitch})
+            assert _linear(rows=1, dtype=dtype, pitch=p) in want
+            assert _pointwise("lbp_dropout", rows=1, dtype=dtype, pitch=p) in want
+            assert _pointwise("lbp_linear_grad", rows=1, dtype=dtype, pitch=p) in want
