@@ -31,6 +31,8 @@ static __int128 extent(const Steps3& s, int C) {
 static int check_numbers(int64_t first, const Steps3& s, int C) {
   return first + extent(s, C) > kMostElements ? LBP_ERR_SHAPE : LBP_OK;
 }
+// Bytes of a tensor's places fit 64 bits with room to spare: nothing that exists is larger.
+constexpr __int128 kMostPlaces = static_cast<__int128>(1) << 58;
 static Steps3 along_rows(long long rows, int64_t pitch) { return Steps3{{rows, 0, 0}, {pitch, 0, 0}}; }
 static Steps3 along_grid(int B, int H, int W, const lbp_view& v) { return Steps3{{B, H, W}, {v.image, v.row, v.token}}; }
 
@@ -38,11 +40,12 @@ static int check_rows(long long rows, int C, int dtype) {
   if (dtype != LBP_F32 && dtype != LBP_BF16) return LBP_ERR_DTYPE;
   if (rows < 0 || rows > (1ll << 40) || C <= 0 || C > (1 << 30)) return LBP_ERR_SHAPE;
   if ((static_cast<long long>(C) * elem_size(dtype)) % 16 != 0) return LBP_ERR_ALIGN;
-  return LBP_OK;
+  return extent(along_rows(rows, C), C) > kMostPlaces ? LBP_ERR_SHAPE : LBP_OK;
 }
-static int check_pitch(int64_t pitch, int C, int dtype) {
+static int check_pitch(long long rows, int64_t pitch, int C, int dtype) {
   if (pitch == 0) return LBP_OK;
   if (pitch < C || pitch >= (int64_t{1} << 40) / elem_size(dtype)) return LBP_ERR_SHAPE;   // (a tensor map's stride: 2^40 bytes)
+  if (extent(along_rows(rows, pitch), C) > kMostPlaces) return LBP_ERR_SHAPE;
   return (pitch * elem_size(dtype)) % 16 != 0 ? LBP_ERR_ALIGN : LBP_OK;
 }
 static bool in_quads(int64_t v, int dtype) { return v % (dtype == LBP_BF16 ? 8 : 4) == 0; }
@@ -130,7 +133,7 @@ static int check_pointwise(const void* a, const void* b, bool need_b, const void
   if (int s = check_epilogue(e, dtype)) return s;
   if (int s = check_numbers(e.first, along_rows(rows, e.number.token ? e.number.token : C), C)) return s;
   for (int64_t v : {p.x, p.residual, p.y, p.z})
-    if (int s = check_pitch(v, C, dtype)) return s;
+    if (int s = check_pitch(rows, v, C, dtype)) return s;
   if (rows == 0) return LBP_OK;
   if (a == nullptr || out == nullptr || (need_b && b == nullptr)) return LBP_ERR_NULL;
   if (!aligned16(a) || !aligned16(b) || !aligned16(out)) return LBP_ERR_ALIGN;
@@ -150,14 +153,14 @@ static int check_shape(int B, int H, int W, int C, int k, int dtype) {
   if (!fits_grid(H, W)) return LBP_ERR_SHAPE;
   return check_rows(static_cast<long long>(B) * H * W, C, dtype);
 }
-static int check_grid_view(const lbp_view& v, int C, int dtype) {
+static int check_grid_view(const lbp_view& v, int B, int H, int W, int C, int dtype) {
   if (v.image == 0 && v.row == 0 && v.token == 0) return LBP_OK;
   if (v.image <= 0 || v.row <= 0 || v.token < C) return LBP_ERR_SHAPE;
   for (int64_t s : {v.image, v.row, v.token}) {
     if (s >= (int64_t{1} << 40) / elem_size(dtype)) return LBP_ERR_SHAPE;
     if ((s * elem_size(dtype)) % 16 != 0) return LBP_ERR_ALIGN;
   }
-  return LBP_OK;
+  return extent(along_grid(B, H, W, v), C) > kMostPlaces ? LBP_ERR_SHAPE : LBP_OK;
 }
 
 // g_z = drop(g_y) act'(z) of a token grid into a dense tensor.
@@ -234,9 +237,9 @@ int lbp_linear(const void* x, const void* W, const void* bias, const void* resid
   if (int s = check_rows(rows, Cout, dtype)) return s;
   if (int s = check_epilogue(e, dtype)) return s;
   if (int s = check_numbers(e.first, along_rows(rows, e.number.token ? e.number.token : Cout), Cout)) return s;
-  if (int s = check_pitch(p.x, Cin, dtype)) return s;
+  if (int s = check_pitch(rows, p.x, Cin, dtype)) return s;
   for (int64_t v : {p.residual, p.y, p.z})
-    if (int s = check_pitch(v, Cout, dtype)) return s;
+    if (int s = check_pitch(rows, v, Cout, dtype)) return s;
   if (rows == 0) return LBP_OK;
   if (x == nullptr || W == nullptr || y == nullptr) return LBP_ERR_NULL;
   for (const void* q : {x, W, bias, residual, static_cast<const void*>(y), static_cast<const void*>(z),
@@ -318,7 +321,7 @@ int lbp_project_grad(const void* g_y, const void* z, void* t_hat, int B, int H, 
   if (int s = check_epilogue(e, dtype)) return s;
   if (int s = check_numbers(e.first, along_grid(B, H, W, resolve_view(&e.number, H, W, C)), C)) return s;
   if (view != nullptr)
-    if (int s = check_grid_view(*view, C, dtype)) return s;
+    if (int s = check_grid_view(*view, B, H, W, C, dtype)) return s;
   BasisPlan plan;
   if (int s = make_basis_plan(k, set, r, &plan)) return s;
   if (!aligned16(g_y) || !aligned16(z) || !aligned16(t_hat) || !aligned16(ws)) return LBP_ERR_ALIGN;
@@ -363,7 +366,7 @@ int lbp_backward_act(const void* x, const void* x_hat, const void* g_y, const vo
     return LBP_ERR_SHAPE;
   if (!in_quads(grad->first_extra, dtype) || !in_quads(grad->number_extra, dtype)) return LBP_ERR_ALIGN;
   if (n_extra > 0)
-    if (int s = check_pitch(ex->gy_extra_pitch, C, dtype)) return s;
+    if (int s = check_pitch(n_extra, ex->gy_extra_pitch, C, dtype)) return s;
   // the call as it is, for what is wrong with it apart from the epilogue
   if (int s = backward_ex_call(x, x_hat, g_y, W, g_x, g_W, layer, set, r, ex, ws, ws_bytes, stream, true)) return s;
   const size_t need = lbp_workspace_bytes_act(layer, r, ex, x_hat != nullptr);

@@ -296,3 +296,14 @@ def test_pitches_past_a_tensor_maps_stride_are_refused(dtype, es):
             assert _linear(rows=1, dtype=dtype, pitch=p) in want
             assert _pointwise("lbp_dropout", rows=1, dtype=dtype, pitch=p) in want
             assert _pointwise("lbp_linear_grad", rows=1, dtype=dtype, pitch=p) in want
+
+
+def test_tensors_past_2_58_elements_are_refused():
+    """Nothing that large exists; rows times channels or a pitch would run over the sums of sizes and places."""
+    assert _linear(rows=1 << 40, Cout=1 << 20, n=1 << 60) == _linear(rows=1 << 40, Cin=1 << 20, n=1 << 60) == SHAPE
+    assert B._lib().lbp_linear_workspace_bytes(1 << 40, 1 << 20, 64, lbp.LBP_BF16) == 0
+    for name in ("lbp_dropout", "lbp_linear_grad"):
+        assert _pointwise(name, rows=1 << 40, Cc=1 << 27) == SHAPE
+        assert _pointwise(name, rows=1 << 40, Cc=64, pitch=B.Pitches(x=1 << 30)) == SHAPE
+    assert _linear(rows=1 << 40, pitch=B.Pitches(x=1 << 30), n=1 << 60) == SHAPE
+    assert _project(B_=1 << 29, H=1, W=1, view=B.View(1 << 38, 64, 64), n=1 << 60) == SHAPE
