@@ -337,7 +337,7 @@ typedef struct {
   uint64_t* used;
   /* Number of an element: of element c of row i, first + i * number.token + c; of
    * element (b, h, w, c) of a token grid, first + b * number.image + h * number.row +
-   * w * number.token + c.  All three zero: dense.  Multiples of 8 with bf16 data, of 4
+   * w * number.token + c.  All three zero: dense; number.token alone may not be.  Multiples of 8 with bf16 data, of 4
    * with fp32.  No element's number may reach 2^62 (LBP_ERR_SHAPE). */
   int64_t first;
   lbp_view number;

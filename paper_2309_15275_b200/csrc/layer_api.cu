@@ -55,6 +55,7 @@ static int check_epilogue(const lbp_epilogue& e, int dtype) {
   if (e.first < 0 || e.first >= kMostElements) return LBP_ERR_SHAPE;
   for (int64_t v : {e.number.image, e.number.row, e.number.token})
     if (v < 0 || v >= (int64_t{1} << 50)) return LBP_ERR_SHAPE;
+  if (e.number.token == 0 && (e.number.image != 0 || e.number.row != 0)) return LBP_ERR_SHAPE;   // (would read as dense)
   for (int64_t v : {e.first, e.number.image, e.number.row, e.number.token})
     if (!in_quads(v, dtype)) return LBP_ERR_ALIGN;
   if (((reinterpret_cast<uintptr_t>(e.seed_dev) | reinterpret_cast<uintptr_t>(e.offset_dev) |

@@ -307,3 +307,11 @@ def test_tensors_past_2_58_elements_are_refused():
         assert _pointwise(name, rows=1 << 40, Cc=64, pitch=B.Pitches(x=1 << 30)) == SHAPE
     assert _linear(rows=1 << 40, pitch=B.Pitches(x=1 << 30), n=1 << 60) == SHAPE
     assert _project(B_=1 << 29, H=1, W=1, view=B.View(1 << 38, 64, 64), n=1 << 60) == SHAPE
+
+
+@pytest.mark.parametrize("number", [B.View(4096, 0, 0), B.View(0, 64, 0), B.View(4096, 64, 0)])
+def test_a_numbering_without_its_innermost_stride_is_refused(number):
+    """All three zero is dense; a zero for the tokens alone read as dense too, whatever the others said."""
+    ep = _ep(p=0.5, number=number)
+    assert _linear(ep=ep) == _pointwise("lbp_dropout", ep=ep) == _pointwise("lbp_linear_grad", ep=ep) == SHAPE
+    assert _project(ep=ep) == _backward(ep=ep) == SHAPE
