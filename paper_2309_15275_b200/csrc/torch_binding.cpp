@@ -762,7 +762,9 @@ PyObject* py_linear_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !parse_tensor(a[10], &c.out) || !parse_tensor(a[11], &c.z) || !parse_tensor(a[12], &c.ws) ||
       !on_current_device(c.x) || !use_rng(rng, c.x.get_device(), &e))
     return not_handled();
-  c.save_z = a[9] == Py_True;
+  const int save_z = PyObject_IsTrue(a[9]);
+  if (save_z < 0) return nullptr;
+  c.save_z = save_z == 1;
   const int s = without_gil([&] { return run_linear(&c, e); });
   if (s < 0) return not_handled();
   return s != LBP_OK ? PyLong_FromLong(s) : c.z.defined() ? pair(c.out, c.z) : THPVariable_Wrap(c.out);

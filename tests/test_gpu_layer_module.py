@@ -80,3 +80,15 @@ def test_tangents_are_refused_and_not_lost(dev, epilogue, frozen, with_grad):
                 call()
         assert layer(x, residual=r).shape == x.shape     # without one it goes on as ever
     assert torch.cuda.default_generators[0].get_offset() == before + (4 if epilogue.get("dropout") else 0)
+
+
+def test_save_z_is_any_truth_value(dev):
+    """A 1 or a numpy truth value asks for z as True does (and is not answered with y alone, which unpacks into rows)."""
+    import numpy as np
+    x, w = _normal((2, 64), 1.0, torch.float32, 1), _normal((32, 64), 1.0, torch.float32, 2)
+    y, z = lbp.lbp_linear(x, w, activation="relu", save_z=True)
+    for yes in (1, np.True_):
+        got = lbp.lbp_linear(x, w, activation="relu", save_z=yes)
+        assert isinstance(got, tuple) and torch.equal(got[0], y) and torch.equal(got[1], z)
+    for no in (0, np.False_, None):
+        assert torch.equal(lbp.lbp_linear(x, w, activation="relu", save_z=no), y)
