@@ -75,7 +75,7 @@ class LbpLinear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None) -> torch.Tensor:
         H, W = self.grid or (0, 0)
-        p = self.dropout if self.training else 0.0
+        p = float(self.dropout) if self.training else 0.0
         if self.activation is not None or p > 0.0 or residual is not None:
             return _b._native().layer(x, self.weight, self.bias, residual, self.k, self.bases, self.save_projected,
                                       H, W, self.activation, p)

@@ -315,3 +315,15 @@ def test_a_numbering_without_its_innermost_stride_is_refused(number):
     ep = _ep(p=0.5, number=number)
     assert _linear(ep=ep) == _pointwise("lbp_dropout", ep=ep) == _pointwise("lbp_linear_grad", ep=ep) == SHAPE
     assert _project(ep=ep) == _backward(ep=ep) == SHAPE
+
+
+def test_a_modules_dropout_may_be_set_to_a_whole_number():
+    """layer.dropout = 0 switches it off, as it does for torch's own layer."""
+    layer = lbp.LbpLinear(64, 32, 8, [(0, 0)], activation="gelu", dropout=0.1)
+    for p in (0, 1, np.float32(0.5)):
+        layer.dropout = p
+        with pytest.raises(ValueError, match="CUDA"):     # (and nothing is said of the arguments' kinds)
+            layer(torch.zeros(1, 8, 8, 64))
+    layer.dropout = 2
+    with pytest.raises(ValueError, match="CUDA|probability"):
+        layer(torch.zeros(1, 8, 8, 64))
