@@ -370,7 +370,8 @@ int lbp_linear_grad(const void* g_y, const void* z, void* g_z, long long rows, i
 int lbp_dropout(const void* x, const void* residual, void* y, long long rows, int C, int dtype,
                 const lbp_pitches* pitch, const lbp_epilogue* epilogue, void* stream);
 
-/* p(g_z) with g_z = drop(g_y) act'(z): as lbp_project on g_z.  g_y, z (B, H, W, C) with the
+/* p(g_z) with g_z = drop(g_y) act'(z): as lbp_project on the g_z that lbp_linear_grad writes, so rounded to the
+ * data's type before it is projected.  g_y, z (B, H, W, C) with the
  * strides of `view` (NULL: dense), z may be NULL without an activation.
  * ws: >= lbp_project_grad_workspace_bytes(...), 0 = invalid shape. */
 size_t lbp_project_grad_workspace_bytes(int B, int H, int W, int C, int k, int r, int dtype);

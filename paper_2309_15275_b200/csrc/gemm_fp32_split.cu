@@ -965,7 +965,8 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const float* planes,
   }
 }
 
-// How a product is cut: columns of a tile, k-blocks of an item.  The times are those of the form table in gemm_fp32.cu.
+// How a product is cut: columns of a tile, k-blocks of an item.  The times are those of the form table in gemm_fp32.cu, for 148
+// SMs (the workspace's size, which follows from this, is asked for without a device).
 struct Cut {
   int bn, chunks;
 };

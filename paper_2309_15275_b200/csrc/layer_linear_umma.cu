@@ -14,11 +14,11 @@
 // channels, or z and y of 32.  The residual is read 32 bytes (a sector) a thread.
 //
 // What bounds it, at 32768 tokens 768 -> 3072 and 1965 MHz: the operands' way from L2 (1.2 GB: 93 us without any
-// store, 1.66 PFLOP/s), which the stores share (y 112, z too 135), and with GELU and dropout the epilogue's arithmetic
-// (26 instructions an element; 151); long runs the power cap (175 at 1.4 GHz).  Tried before the arithmetic was what it
-// is now, against 116, 144 and 171 us: a 32-byte store a thread without shared memory (112, 149, 175, and 48 -> 192
+// store, 1.66 PFLOP/s), which the stores share (y 116, z too 140), and with GELU and dropout the epilogue's arithmetic
+// (27 instructions an element; 163); long runs the power cap (189 at 1.4 GHz).  200704 tokens 48 -> 192, one k-block a tile: 28
+// us without an activation, 36 with GELU.  Tried before the arithmetic was what it is now, against 116, 144 and 171 us: a 32-byte store a thread without shared memory (112, 149, 175, and 48 -> 192
 // channels 46 instead of 43), a bulk copy per row by its thread (116, 201, 297), twelve warps (116, 142, 185).  z
-// in a pass of its own: 139 and 155 now, 48 -> 192 channels 40 instead of 37, GELU without dropout 134 instead of 138.
+// in a pass of its own, against 135 and 151: 139 and 155, 48 -> 192 channels 40 instead of 37, GELU without dropout 134 instead of 138.
 #include "layer_math.cuh"
 #include "ptx_sm100.cuh"
 

@@ -1,10 +1,20 @@
 // The elementwise part of a layer's epilogue: activations, their derivatives, and dropout
 // from a counter-based generator.
 //
-// The activations go through the approximate exponential and reciprocal of the special-function unit (2^-22 of their
-// result), two numbers at a time, and polynomials of two lengths: for results that are rounded to bf16, and for fp32
-// (FINE).  They take +-infinity to the limit and keep NaN.  (CUDA's erfcf and expf in their place cost the fp32
-// gradient of 16384 x 3072 GELUs 107 us, 154 with dropout, instead of 88 and 92.)
+// The activations go through the approximate exponential and reciprocal of the special-function unit (2^-22 and 2^-23 of
+// their results), two numbers at a time, and polynomials of two lengths: for results that are rounded to bf16, and for fp32
+// (FINE).  They take +-infinity to the limit and keep NaN.  What they are off by before that rounding, relative to the result,
+// evaluated step by step with an exact exponential and reciprocal (GELU from -13 on, its tanh form from -9.5, SiLU from -86; the
+// slopes away from their zeros):
+//                    up to -5     -5 .. -2     from -0.5 on    slopes
+//   GELU, bf16       4.4e-5       3.7e-5       3.7e-5          7.8e-6, 7.5e-6, 4.7e-5
+//   GELU             7.9e-6       1.3e-6       4.3e-7          8.0e-6, 1.3e-6, 7.0e-7
+//   tanh form        1.1e-5       2.2e-6       1.8e-7          1.1e-5, 2.3e-6, 2.0e-6
+//   SiLU             3.9e-6       3.4e-7       1.6e-7          3.9e-6, 3.9e-7, 9.8e-7
+// In the tails that is the exponent u, whose rounding to fp32 moves exp(u) by some |u| 2^-24 of itself.  A reciprocal below
+// 2^-126 is 0, so SiLU is from -87.4 on and the tanh form from -10.1 (below 6e-37).
+// CUDA's erfcf and expf in their place cost the fp32 gradient of 16384 x 3072 GELUs 107 us, 154 with dropout, instead of 89
+// and 97.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -349,38 +359,33 @@ __device__ __forceinline__ void gradient(const uint4 (&g)[U], const uint4 (&z)[U
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    float v[V::N];
     if constexpr (V::N == 8) {
       uint32_t m[4] = {};
       if constexpr (DROP) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) m[j] = kept_halves(w[4 * u + j], d);
       }
-      masked_gradient<ACT, DROP>(g[u], z[u], m, d, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) out[u][j] = v[j];
-      continue;
-    }
-    V::unpack(g[u], v);
-    if constexpr (ACT != LBP_ACT_NONE) {
-      float x[V::N];
-      V::unpack(z[u], x);
-#pragma unroll
-      for (int j = 0; j < V::N; j += 2) {
-        times_slope2<ACT, true>(v[j], v[j + 1], x[j], x[j + 1]);
-      }
-    }
-    if constexpr (DROP) {
-      const bool upper = V::N == 4 && (number[u] & 4u) != 0;
-#pragma unroll
-      for (int j = 0; j < V::N; j += 2) {
-        out[u][j] = out[u][j + 1] = 0.f;
-        const uint32_t word = V::N == 8 ? w[4 * u + j / 2] : upper ? w[4 * u + 2 + j / 2] : w[4 * u + j / 2];
-        add_kept2(out[u][j], out[u][j + 1], v[j], v[j + 1], word, d);
-      }
+      masked_gradient<ACT, DROP>(g[u], z[u], m, d, out[u]);
     } else {
+      float v[4];
+      V::unpack(g[u], v);
+      if constexpr (ACT != LBP_ACT_NONE) {
+        float x[4];
+        V::unpack(z[u], x);
 #pragma unroll
-      for (int j = 0; j < V::N; ++j) out[u][j] = v[j];
+        for (int j = 0; j < 4; j += 2) times_slope2<ACT, true>(v[j], v[j + 1], x[j], x[j + 1]);
+      }
+      const bool upper = (number[u] & 4u) != 0;
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        if constexpr (DROP) {
+          out[u][j] = out[u][j + 1] = 0.f;
+          add_kept2(out[u][j], out[u][j + 1], v[j], v[j + 1], upper ? w[4 * u + 2 + j / 2] : w[4 * u + j / 2], d);
+        } else {
+          out[u][j] = v[j];
+          out[u][j + 1] = v[j + 1];
+        }
+      }
     }
   }
 }

@@ -1,16 +1,16 @@
 // out = residual + drop(a) act'(z): dropout on its own, and the gradient of a layer's epilogue.
 //
 // One pass; a thread has kVectors vectors of 16 bytes of each tensor, 256 threads apart, and asks for all of
-// them before it computes.  32768 x 3072 of bf16: GELU's gradient 89 us, 604 MB at 6.8 TB/s; with p = 0.1 106 us,
-// bound by issue (26 instructions an element, ten of them for the numbers).
+// them before it computes.  32768 x 3072 of bf16: GELU's gradient 89 us, 604 MB at 6.8 TB/s; with p = 0.1 118 us
+// (28 instructions an element, ten of them for the numbers, in 65 % of the issue slots).
 #include "layer_math.cuh"
 
 namespace lbp {
 namespace layer {
 
 // Vectors of a thread: with more, more loads are under way and more Philox calls share a key's additions; with
-// fewer, more blocks.  32768 x 3072 of bf16 with p = 0.1, 2 / 3 / 4 vectors: GELU's gradient 108 / 106 / 112 us, SiLU's
-// 95 / 98 / 92, without an activation 72 / 68 / 65.  (A bound on the registers, for more blocks to an SM, cost 15 %.)
+// fewer, more blocks.  32768 x 3072 of bf16 with p = 0.1, 2 / 3 / 4 vectors: GELU's gradient 122 / 120 / 122 us, SiLU's
+// 104 / 105 / 101, without an activation 74 / 70 / 68.  (A bound on the registers, for more blocks to an SM, cost 15 %.)
 constexpr int kVectors = 3;
 
 // n / d for n < 2^31 without a division: magic numbers from the host (Granlund and Montgomery 1994).

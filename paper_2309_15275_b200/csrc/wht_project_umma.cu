@@ -37,8 +37,9 @@
 //
 // GRAD: tensor 0 is g_z = drop(g_y) act'(z), which is never in memory.  A stage holds the boxes of g_y and z; sixteen
 // more warps, in two sets that take turns, overwrite g_y with g_z where it lies (both have the same swizzle, so a thread's 16 bytes of
-// the one lie like those of the other) before the tensor core reads it.  One epilogue group is enough: what bounds it is
-// the arithmetic of those warps.
+// the one lie like those of the other) before the tensor core reads it.  One epilogue group is enough: what takes the time is
+// what those warps do once a stage is there, the numbers' ten dependent rounds and the slope, at 55 % of the issue slots.
+// 128 x 16 x 16 tokens of 3072 channels at rank 8: ReLU 68 us (the memory's 65), GELU 96, dropout alone 89, GELU and dropout 142.
 #include <cuda_bf16.h>
 
 #include "layer_math.cuh"

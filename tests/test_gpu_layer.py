@@ -7,9 +7,9 @@ a result, relative to it):
         twice that
   y     u |y| + s (1.13 dz + da) + 2^-23 (|r| + |d|): dz the second part of z's bound (1.13 bounds the
         activations' slopes), da the error of the activation itself, s the scale of drop(), the rest the sum
-        with the residual.  da: 2^-13 |act| + 2^-20 for bf16 data, whose activations are approximated to 3.7e-5 of
-        the smaller of Phi and 1 - Phi and to a few units of 2^-22 otherwise, 2^-20 (1 + z^2) |act| + 2^-24 for
-        fp32 (CUDA's functions: a few units of 2^-24, times z^2 for the rounding of the exponent)
+        with the residual.  da: 2^-13 |act| + 2^-20 for bf16 data, whose GELU is approximated to 3.7e-5 of Phi(-|z|)
+        and the others to a few units of 2^-22, 2^-20 (1 + z^2) |act| + 2^-24 for
+        fp32 (a few units of 2^-22, and of 2^-24 times z^2 for the rounding of the exponent)
   g_z   (u + 2^-21) |g_z| + s |g_y| ds, ds = 2^-14 (bf16), 2^-19 (fp32) the error of a slope (the parts of a
         slope are at most z^2 exp(-z^2/2) times a rounding of 2^-24 each)
 """
