@@ -600,6 +600,21 @@ PyObject* wrap_like(const Tensor& y, PyObject* const* a, int n) {
   return out;
 }
 
+// LinearFunction under autocast too: the backward pass wants x, weight and g_y of one type, which is that of y, so x and
+// weight are brought to it first.  (The product rounds them to autocast's type either way.)
+Tensor plain_layer(Tensor x, Tensor weight, const Tensor& bias, int k, const std::vector<int64_t>& bases, bool projected, int H,
+                   int W) {
+  if (x.is_cuda() && at::autocast::is_autocast_enabled(at::kCUDA)) {
+    const at::ScalarType t = at::autocast::get_autocast_dtype(at::kCUDA);
+    const at::ScalarType of_y = bias.defined() ? c10::promoteTypes(t, bias.scalar_type()) : t;
+    if (dtype_code(of_y) >= 0)
+      for (Tensor* v : {&x, &weight})
+        if (v->is_floating_point() && v->scalar_type() != at::kDouble) *v = v->to(of_y);   // (torch's autocast passes doubles over)
+  }
+  return LinearFunction::apply(x, weight, bias.defined() ? std::optional<Tensor>(bias) : std::nullopt, static_cast<int64_t>(k),
+                               bases, projected, static_cast<int64_t>(H), static_cast<int64_t>(W));
+}
+
 // linear(x, weight, bias | None, k, bases, save_projected, H, W) -> y
 PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -622,9 +637,7 @@ PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Tensor y;
   {
     pybind11::gil_scoped_release no_gil;
-    y = LinearFunction::apply(x, weight, bias.defined() ? std::optional<Tensor>(bias) : std::nullopt,
-                              static_cast<int64_t>(k), flat, projected, static_cast<int64_t>(H),
-                              static_cast<int64_t>(W));
+    y = plain_layer(x, weight, bias, k, flat, projected, H, W);
   }
   return wrap_like(y, a, 3);
   END_HANDLE_TH_ERRORS
@@ -1146,8 +1159,7 @@ PyObject* py_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (at::GradMode::is_enabled())
       for (const Tensor* v : {&x, &weight, &bias, &residual}) backward |= v->defined() && v->requires_grad();
     if (stream.defined() && act == LBP_ACT_NONE && p == 0.0)   // nothing else follows the product: the plain layer's
-      y = LinearFunction::apply(x, weight, opt(bias), static_cast<int64_t>(k), flat, projected, static_cast<int64_t>(H),
-                                static_cast<int64_t>(W));
+      y = plain_layer(x, weight, bias, k, flat, projected, H, W);
     else if (backward)
       y = LayerFunction::apply(x, weight, opt(bias), opt(residual), static_cast<int64_t>(k), flat, projected,
                                static_cast<int64_t>(H), static_cast<int64_t>(W), static_cast<int64_t>(act), p);

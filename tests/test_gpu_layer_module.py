@@ -92,3 +92,59 @@ def test_save_z_is_any_truth_value(dev):
         assert isinstance(got, tuple) and torch.equal(got[0], y) and torch.equal(got[1], z)
     for no in (0, np.False_, None):
         assert torch.equal(lbp.lbp_linear(x, w, activation="relu", save_z=no), y)
+
+
+AUTOCAST = [(b, i) for b in (None, torch.bfloat16, torch.float32) for i in (torch.bfloat16, torch.float32)]
+
+
+@pytest.mark.parametrize("bias,dtype", AUTOCAST)
+@pytest.mark.parametrize("epilogue", EPILOGUES)
+@pytest.mark.parametrize("cls", [None, 1, 2])
+def test_a_residual_stream_under_autocast_with_any_bias_and_input(dev, epilogue, cls, bias, dtype):
+    """An fp32 stream onto a layer of fp32 weights: whatever the layer's input and bias are, it is torch's sum of the two."""
+    shape = (3, 8, 8) if cls is None else (3, cls + 64)
+    layer = lbp.LbpLinear(64, 96, K, BASES, device=dev, dtype=torch.float32, bias=bias is not None,
+                          grid=None if cls is None else (8, 8), **epilogue)
+    if bias is not None:
+        layer.bias = torch.nn.Parameter(_normal((96,), 0.3, bias, 9))
+    x = _normal(shape + (64,), 1.0, dtype, 1).requires_grad_()
+    r = _normal(shape + (96,), 1.0, torch.float32, 2).requires_grad_()
+    g = _normal(shape + (96,), 1.0, torch.float32, 3)
+    leaves = (x, r) + tuple(layer.parameters())
+
+    def run(step):
+        torch.manual_seed(11)
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            y = step()
+        return y, torch.autograd.grad(y, leaves, g)
+
+    want, want_grads = run(lambda: r + layer(x))
+    y, grads = run(lambda: layer(x, residual=r))
+    assert y.dtype == torch.float32 and torch.equal(y, want)
+    assert torch.equal(grads[1], g) and all(torch.equal(a, b) and a.dtype == v.dtype for a, b, v in zip(grads, want_grads, leaves))
+
+
+@pytest.mark.parametrize("bias,dtype", AUTOCAST)
+@pytest.mark.parametrize("cls,projected", [(None, False), (None, True), (1, False), (2, False)])
+def test_the_plain_layer_trains_under_autocast_with_any_bias_and_input(dev, cls, projected, bias, dtype):
+    """y is torch's: the product in bf16, the bias added by torch's rules.  The backward pass is the library's on operands of
+    y's type."""
+    shape = (3, 8, 8) if cls is None else (3, cls + 64)
+    layer = lbp.LbpLinear(64, 96, K, BASES, device=dev, dtype=torch.float32, bias=bias is not None, save_projected=projected,
+                          grid=None if cls is None else (8, 8))
+    if bias is not None:
+        layer.bias = torch.nn.Parameter(_normal((96,), 0.3, bias, 9))
+    x = _normal(shape + (64,), 1.0, dtype, 1).requires_grad_()
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        y = layer(x)
+        want = torch.matmul(x, layer.weight.t())
+        want = want if bias is None else want + layer.bias
+    assert y.dtype == want.dtype and torch.equal(y, want)
+    g = _normal(y.shape, 1.0, y.dtype, 3)
+    grads = torch.autograd.grad(y, (x,) + tuple(layer.parameters()), g)
+    same = lbp.LbpLinear(64, 96, K, BASES, device=dev, dtype=y.dtype, bias=bias is not None, save_projected=projected, grid=layer.grid)
+    same.load_state_dict({n: v.to(y.dtype) for n, v in layer.state_dict().items()})
+    xs = x.detach().to(y.dtype).requires_grad_()
+    ref = torch.autograd.grad(same(xs), (xs,) + tuple(same.parameters()), g)
+    for a, b, v in zip(grads, ref, (x,) + tuple(layer.parameters())):
+        assert a.dtype == v.dtype and torch.equal(a, b.to(v.dtype))
