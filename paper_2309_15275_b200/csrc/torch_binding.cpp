@@ -600,16 +600,18 @@ PyObject* wrap_like(const Tensor& y, PyObject* const* a, int n) {
   return out;
 }
 
-// LinearFunction under autocast too: the backward pass wants x, weight and g_y of one type, which is that of y, so x and
-// weight are brought to it first.  (The product rounds them to autocast's type either way.)
+// LinearFunction under autocast too: the backward pass wants x, weight and g_y of one type, which is that of y, so where
+// one is to follow x and weight are brought to it first.  (The product rounds them to autocast's type either way.  Not by
+// autocast's cache, whose entry may have been made under no_grad.)
 Tensor plain_layer(Tensor x, Tensor weight, const Tensor& bias, int k, const std::vector<int64_t>& bases, bool projected, int H,
                    int W) {
-  if (x.is_cuda() && at::autocast::is_autocast_enabled(at::kCUDA)) {
+  const bool backward = at::GradMode::is_enabled() && (x.requires_grad() || weight.requires_grad() || (bias.defined() && bias.requires_grad()));
+  if (backward && x.is_cuda() && at::autocast::is_autocast_enabled(at::kCUDA)) {
     const at::ScalarType t = at::autocast::get_autocast_dtype(at::kCUDA);
     const at::ScalarType of_y = bias.defined() ? c10::promoteTypes(t, bias.scalar_type()) : t;
     if (dtype_code(of_y) >= 0)
       for (Tensor* v : {&x, &weight})
-        if (v->is_floating_point() && v->scalar_type() != at::kDouble) *v = v->to(of_y);   // (torch's autocast passes doubles over)
+        if (v->is_floating_point() && v->scalar_type() != at::kDouble) *v = v->to(of_y);   // (autocast passes doubles over)
   }
   return LinearFunction::apply(x, weight, bias.defined() ? std::optional<Tensor>(bias) : std::nullopt, static_cast<int64_t>(k),
                                bases, projected, static_cast<int64_t>(H), static_cast<int64_t>(W));

@@ -148,3 +148,22 @@ def test_the_plain_layer_trains_under_autocast_with_any_bias_and_input(dev, cls,
     ref = torch.autograd.grad(same(xs), (xs,) + tuple(same.parameters()), g)
     for a, b, v in zip(grads, ref, (x,) + tuple(layer.parameters())):
         assert a.dtype == v.dtype and torch.equal(a, b.to(v.dtype))
+
+
+@pytest.mark.parametrize("epilogue", EPILOGUES)
+@pytest.mark.parametrize("bias", [False, True])
+def test_a_look_without_gradients_first_loses_none_under_autocast(dev, epilogue, bias):
+    """In one autocast context: evaluation under no_grad, then a training step of the same layer."""
+    layer = lbp.LbpLinear(64, 96, K, BASES, device=dev, dtype=torch.float32, bias=bias, **epilogue)
+    x = _normal((2, 8, 8, 64), 1.0, torch.float32, 1).requires_grad_()
+    leaves = (x,) + tuple(layer.parameters())
+    grads = []
+    for look in (False, True):
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            if look:
+                with torch.no_grad():
+                    layer(x)
+            torch.manual_seed(5)
+            y = layer(x)
+        grads.append(torch.autograd.grad(y, leaves, torch.ones_like(y)))
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
